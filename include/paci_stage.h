@@ -286,6 +286,123 @@ int paci_stage_backward_static(paci_stage* h, int mb, const void* dev_grad_out, 
  * t + 1 while no update was skipped. */
 int paci_stage_step(paci_stage* h, int* new_version);
 
+/* ---- attention operators --------------------------------------------------------
+ * Single operators on device buffers, beside the ones a stage runs inside its
+ * blocks (the paper's stages use neither option). Work is enqueued on
+ * `hip_stream` (NULL: the null stream), which must belong to the current
+ * device, as must every buffer. Nothing is allocated, cleared or synchronized,
+ * so the calls can be captured into a graph. Rows: `ld_*` is a row stride in
+ * elements, at least the row's length (it may be smaller for a single row), a
+ * multiple of 16 bytes; row pointers are 16-byte aligned. Buffers of one call
+ * may overlap only where this is said. Gradients of parameters (dev_g_*) are
+ * added to what the buffer holds, like a stage's G, in an order that does not
+ * depend on timing. Workspaces hold nothing between calls; calls that can
+ * overlap in time need one each. On a negative status nothing was enqueued
+ * (PACI_E_HIP excepted: see paci_last_hip_error(NULL)). */
+
+/* Norms and rotation of the query and key heads, in one pass: per token and
+ * head, n = x / sqrt(mean(x^2) + eps) * gain (norm = 1; gains of head_dim fp32,
+ * one for all query heads and one for all key heads; n = x without), then the
+ * first rope_dims elements of n in pairs, pair i turned by the angle
+ * position * freq[i]: (a, b) -> (a cos - b sin, a sin + b cos). The other
+ * elements pass through. */
+enum paci_rope_pairs {
+  PACI_ROPE_HALF = 0,    /* pair i is elements i and i + rope_dims / 2 */
+  PACI_ROPE_ADJACENT = 1 /* pair i is elements 2 i and 2 i + 1 */
+};
+typedef struct paci_qk_shapes {
+  int32_t dtype;      /* enum paci_dtype, of x, y and their gradients */
+  int32_t tokens;     /* rows (0: the call does nothing) */
+  int32_t seq;        /* without dev_pos, row t is at position t % seq (>= 1) */
+  int32_t q_heads;    /* a row is q_heads query heads, then k_heads key heads */
+  int32_t k_heads;    /* (either may be 0; 16384 together at most) */
+  int32_t head_dim;   /* multiple of 16, at most 256 */
+  int32_t norm;       /* 1: RMS norm with gains; 0: rotation only */
+  float eps;          /* of the norm, >= 0 */
+  int32_t rope_dims;  /* rotated elements of a head, a multiple of 16; 0: norm only */
+  int32_t rope_pairs; /* enum paci_rope_pairs */
+} paci_qk_shapes;
+
+/* host_freq[i] = theta^(-2 i / rope_dims), i < rope_dims / 2: the usual
+ * frequencies in radians per position. Host only. E_INVAL: theta not positive
+ * and finite, rope_dims odd or below 2, null pointer. */
+int paci_rope_freqs(double theta, int rope_dims, double* host_freq);
+
+/* y = rot(norm(x)). dev_x and dev_y: [tokens, (q_heads + k_heads) * head_dim]
+ * with row strides; dev_y may be dev_x with the same stride. dev_q_gain /
+ * dev_k_gain: [head_dim] fp32 (ignored without norm; NULL without heads of
+ * the kind). dev_pos: int32 positions [tokens], any value, or NULL. dev_freq:
+ * [rope_dims / 2] fp64, radians per position; the angle is formed in 64 bits,
+ * so far positions keep it (ignored when rope_dims = 0).
+ * Errors: E_INVAL (null or misaligned pointer, stride, negative or impossible
+ * size, neither norm nor rotation), E_UNSUPPORTED (head_dim, rope_dims, dtype
+ * as above), E_HIP. */
+int paci_qk_norm_rope_forward(const paci_qk_shapes* s, const void* dev_x, int64_t ld_x, const float* dev_q_gain,
+                              const float* dev_k_gain, const int32_t* dev_pos, const double* dev_freq, void* dev_y,
+                              int64_t ld_y, void* hip_stream);
+
+/* Its backward: dev_dx = dL/dx from dev_dy = dL/dy, the forward's x, gains,
+ * positions and frequencies. dev_g_q_gain / dev_g_k_gain ([head_dim] fp32,
+ * nullable; NULL without norm) += the gains' gradients; dev_g_bias
+ * ([(q_heads + k_heads) * head_dim] fp32, nullable) += the column sums of
+ * dL/dx, the bias gradient of the projection that made x. dev_dx may be dev_dy
+ * with the same stride, not dev_x. Without norm, dev_x is not read. dev_ws:
+ * paci_qk_norm_rope_workspace bytes, 16-byte aligned (not read without norm
+ * and dev_g_bias). Errors as above, and E_NOMEM (workspace too small). */
+int paci_qk_norm_rope_workspace(const paci_qk_shapes* s, size_t* bytes);
+int paci_qk_norm_rope_backward(const paci_qk_shapes* s, const void* dev_x, int64_t ld_x, const void* dev_dy,
+                               int64_t ld_dy, const float* dev_q_gain, const float* dev_k_gain, const int32_t* dev_pos,
+                               const double* dev_freq, void* dev_dx, int64_t ld_dx, float* dev_g_q_gain,
+                               float* dev_g_k_gain, float* dev_g_bias, void* dev_ws, size_t ws_bytes,
+                               void* hip_stream);
+
+/* Causal attention with a learned relative position bias: per sequence and head
+ *   o = softmax(q k^T / sqrt(head_dim) + table[bucket(i - j)][head]) v
+ * over the keys j at or before each query i. bucket(n) is the number of
+ * bounds[1 .. n_buckets - 1] at or below min(n, max_distance). Table entries at
+ * or below -1e30 (-inf, the lowest float) hide their distances from that head;
+ * a query with no key left has o = 0 and lse2 = -inf and passes no gradient on.
+ * n_buckets = 0: no bias (table, bounds and their gradient NULL). */
+typedef struct paci_attn_shapes {
+  int32_t dtype;        /* enum paci_dtype, of q, k, v, o and their gradients */
+  int32_t batch, seq;   /* token t = b * seq + s (either 0: the call does nothing) */
+  int32_t n_heads;      /* batch * n_heads at most 65535, seq at most 2^20 */
+  int32_t head_dim;     /* 32, 64 or (bf16) 128 */
+  int32_t n_buckets;    /* 0, or 2 .. 256 */
+  int32_t max_distance; /* 1 .. 512: distances from it on are one */
+} paci_attn_shapes;
+
+/* The usual bounds: bucket n for each distance n below e = n_buckets / 2, then
+ * logarithmic steps, bucket e + k from the first distance at or above
+ * e (max_distance / e)^(k / (n_buckets - e)). host_bounds: int32 [n_buckets].
+ * Host only. E_INVAL: n_buckets < 2, max_distance <= n_buckets / 2, null
+ * pointer; E_UNSUPPORTED: beyond 256 buckets or distance 512. */
+int paci_rel_bounds(int n_buckets, int max_distance, int32_t* host_bounds);
+
+/* dev_q, dev_k, dev_v: [batch * seq, n_heads * head_dim] with row strides (the
+ * thirds of a fused projection, or buffers of their own). dev_table: fp32
+ * [n_buckets, n_heads]. dev_bounds: int32 [n_buckets], ascending (the first is
+ * not read as a bound). dev_o: [batch * seq, n_heads * head_dim], dense.
+ * dev_lse2: fp32 [batch * n_heads, seq], log2 of the sum of 2^(score * log2 e).
+ * Without a bias lse2 sums the probabilities as the products use them (rounded
+ * to the dtype). Errors as for the norms. */
+int paci_attn_forward(const paci_attn_shapes* s, const void* dev_q, int64_t ld_q, const void* dev_k, int64_t ld_k,
+                      const void* dev_v, int64_t ld_v, const float* dev_table, const int32_t* dev_bounds, void* dev_o,
+                      float* dev_lse2, void* hip_stream);
+
+/* Its backward, from dev_do = dL/do (dense like dev_o), the forward's operands,
+ * o and lse2: with P = 2^(score log2 e - lse2) and dS = P (do v^T - rowsum(do o)),
+ * dq = dS k / sqrt(head_dim), dk = dS^T q / sqrt(head_dim), dv = P^T do, and
+ * dev_g_table[b][h] (fp32 [n_buckets, n_heads], nullable) += the sum of dS over
+ * the pairs of bucket b. dq, dk and dv have row strides and must not overlap an
+ * operand. dev_ws: paci_attn_workspace bytes, 16-byte aligned. Errors as above. */
+int paci_attn_workspace(const paci_attn_shapes* s, size_t* bytes);
+int paci_attn_backward(const paci_attn_shapes* s, const void* dev_q, int64_t ld_q, const void* dev_k, int64_t ld_k,
+                       const void* dev_v, int64_t ld_v, const float* dev_table, const int32_t* dev_bounds,
+                       const void* dev_o, const float* dev_lse2, const void* dev_do, void* dev_dq, int64_t ld_dq,
+                       void* dev_dk, int64_t ld_dk, void* dev_dv, int64_t ld_dv, float* dev_g_table, void* dev_ws,
+                       size_t ws_bytes, void* hip_stream);
+
 /* ---- schedule driver --------------------------------------------------------- */
 /* The schedule driver: the event order of Alg. 1 at one stage, each forward
  * issued as soon as admission allows and each update right after the backward
@@ -342,7 +459,7 @@ int paci_stage_updates(paci_stage* h, int32_t* applied, int32_t* skipped);
 /* ---- introspection ------------------------------------------------------------- */
 int paci_stage_counters(const paci_stage* h, paci_counters* out);
 int paci_stage_sync(paci_stage* h);              /* hipStreamSynchronize; E_HIP on failure */
-int paci_last_hip_error(const paci_stage* h);    /* the hipError_t behind the last E_HIP (NULL: of paci_stage_init) */
+int paci_last_hip_error(const paci_stage* h);    /* the hipError_t behind the last E_HIP (NULL: of paci_stage_init and the operator calls) */
 const char* paci_strerror(int status);
 
 /* Kernel timing: while enabled, each kernel launch of the stage is bracketed by

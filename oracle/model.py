@@ -99,8 +99,19 @@ def _merge(o):
     return o.transpose(0, 2, 1, 3).reshape(mu * S, H * dh)
 
 
-def attention_fwd(qkv, mu, S, n_heads, head_dim, keep=None, drop_scale=1.0):
-    """o = softmax(q k^T / sqrt(dh) + causal mask) v for every sequence and head.
+def _bias_matrix(bias, h, S):
+    """[S, S] bias of head h from bias [H, S] by distance (0 above the diagonal); 0.0 for None."""
+    if bias is None:
+        return 0.0
+    i = np.arange(S)
+    return bias[h][np.maximum(i[:, None] - i, 0)]
+
+
+def attention_fwd(qkv, mu, S, n_heads, head_dim, keep=None, drop_scale=1.0, bias=None):
+    """o = softmax(q k^T / sqrt(dh) + bias + causal mask) v for every sequence and head.
+
+    ``bias`` [H, S] (optional) is added by distance; a query whose every key it
+    hides (-inf) has o = 0 and lse = -inf.
 
     With ``keep`` [mu, H, S, S] (dropout on the probabilities) the product
     uses P * keep * drop_scale. Returns o as [T, d] and the per-row
@@ -113,21 +124,24 @@ def attention_fwd(qkv, mu, S, n_heads, head_dim, keep=None, drop_scale=1.0):
     lse = np.empty((mu, n_heads, S))
     for b in range(mu):
         for h in range(n_heads):
-            s = (q[b, h] @ k[b, h].T) * scale
+            s = (q[b, h] @ k[b, h].T) * scale + _bias_matrix(bias, h, S)
             s[future] = -np.inf
             smax = s.max(axis=1, keepdims=True)
+            smax[smax == -np.inf] = 0.0
             e = np.exp(s - smax)
             rowsum = e.sum(axis=1, keepdims=True)
-            P = e / rowsum
+            P = e / np.where(rowsum == 0, 1.0, rowsum)
             if keep is not None:
                 P = P * keep[b, h] * drop_scale
             o[b, h] = P @ v[b, h]
-            lse[b, h] = (smax + np.log(rowsum))[:, 0]
+            with np.errstate(divide="ignore"):
+                lse[b, h] = (smax + np.log(rowsum))[:, 0]
     return _merge(o), lse
 
 
-def attention_bwd(do_, qkv, lse, mu, S, n_heads, head_dim, keep=None, drop_scale=1.0):
-    """Backward of attention_fwd; returns d(qkv) as [T, 3d].
+def attention_bwd(do_, qkv, lse, mu, S, n_heads, head_dim, keep=None, drop_scale=1.0, bias=None):
+    """Backward of attention_fwd; returns d(qkv) as [T, 3d], and with ``bias`` also
+    the sum of dS over the sequences, [H, S, S] (the gradient of the biased scores).
 
     P is rebuilt from q, k and the saved log-sum-exp (it holds no parameter).
     With dP = dO V^T: dV = P^T dO, dS = P * (dP - rowsum(dP * P)),
@@ -140,22 +154,26 @@ def attention_bwd(do_, qkv, lse, mu, S, n_heads, head_dim, keep=None, drop_scale
     scale = 1.0 / math.sqrt(head_dim)
     future = np.triu(np.ones((S, S), dtype=bool), k=1)
     dq, dk, dv = np.empty_like(q), np.empty_like(k), np.empty_like(v)
+    ds_sum = np.zeros((n_heads, S, S)) if bias is not None else None
     for b in range(mu):
         for h in range(n_heads):
-            s = (q[b, h] @ k[b, h].T) * scale
+            s = (q[b, h] @ k[b, h].T) * scale + _bias_matrix(bias, h, S)
             s[future] = -np.inf
-            P = np.exp(s - lse[b, h][:, None])
+            row = lse[b, h][:, None]
+            P = np.exp(s - np.where(row == -np.inf, np.inf, row))
             Mk = 1.0 if keep is None else keep[b, h] * drop_scale
             dv[b, h] = (P * Mk).T @ dO[b, h]
             dP = (dO[b, h] @ v[b, h].T) * Mk
             dS = P * (dP - (dP * P).sum(axis=1, keepdims=True))
             dq[b, h] = (dS @ k[b, h]) * scale
             dk[b, h] = (dS.T @ q[b, h]) * scale
+            if ds_sum is not None:
+                ds_sum[h] += dS
     out = np.empty((mu * S, 3 * d))
     out[:, 0:d] = _merge(dq)
     out[:, d:2 * d] = _merge(dk)
     out[:, 2 * d:3 * d] = _merge(dv)
-    return out
+    return out if ds_sum is None else (out, ds_sum)
 
 
 # ----------------------------------------------------------------------------

@@ -1,9 +1,9 @@
 // Causal multi-head attention, forward and backward, gfx950.
 //
-// q, k and v live side by side in the fused projection qkv [T, 3d] (head h at
-// columns h*dh of each third) and are read in place. Blocks of 64 keys (and
-// of 64 or 32 queries) are staged in LDS, and every product is an MFMA chain
-// in the convention of device_common.hpp.
+// q, k and v are rows of H * dh elements with a row stride each (side by side in
+// the fused projection, or q and k in a buffer of their own) and are read in
+// place. Blocks of 64 keys (and of 64 or 32 queries) are staged in LDS, and every
+// product is an MFMA chain in the convention of device_common.hpp.
 //
 // Forward (one workgroup per (sequence, head, 64 queries); 4 wavefronts of 16
 // queries, heaviest causal blocks first): S^T = K Q^T, so each lane owns one
@@ -31,10 +31,133 @@ constexpr int NT = 256;
 constexpr int BKV = 64;   // keys per block
 constexpr float LOG2E = 1.4426950408889634f;
 
+// Operands: row t of q at q + t * ldq (elements), head h at + h * dh; likewise k and v.
+template <typename T> struct QkvView {
+  const T* q; const T* k; const T* v;
+  int64_t ldq, ldk, ldv;
+};
+// Gradients in the same manner, and where their column sums are added (H * dh floats each, nullable).
+template <typename T> struct GradView {
+  T* q; T* k; T* v;
+  int64_t ldq, ldk, ldv;
+  float* sq; float* sk; float* sv;
+};
+
+// ---- relative position bias -------------------------------------------------------------
+// The score of query i and key j <= i adds table[bucket(i - j)][h], where distances
+// from max_distance on share the last bucket reached. A workgroup serves one head, so
+// its bias is a vector over the distance, built once in LDS in units of log 2:
+//   vec[FRONT + n] = log2(e) * table[bucket(n)][h],  n = 0 .. max_distance, then the
+//   value of max_distance up to n = max_distance + TAIL.
+// A tile of 16 queries and 16 keys at distance 16 D holds distances 16 D - 15 .. 16 D + 15,
+// so tiles of equal D read the same values, and a block whose distances all reach
+// max_distance reads none: one value serves it (`far`).
+// Entries at or below MASKED hide their distances (-inf).
+struct BiasArgs {
+  const float* table;      // [n_buckets][H]
+  const int32_t* bounds;   // first distance of every bucket, ascending
+  int n_buckets, max_distance;
+  float* part;             // dQ workgroups: sums of dS by distance, [heads][query blocks][max_distance + 1], or null
+};
+constexpr int BIAS_FRONT = 80, BIAS_TAIL = 128;   // distances below 0 (masked keys) and above max_distance inside a window
+constexpr float BIAS_MASKED = -1e30f;
+__host__ __device__ __forceinline__ int bias_len(int max_distance) { return BIAS_FRONT + max_distance + BIAS_TAIL; }
+// LDS behind the tiles, floats: the vector, bounds and table column, then (dQ) one vector of sums per wavefront.
+__host__ __device__ __forceinline__ int bias_lds_floats(int max_distance, int n_buckets, int waves) {
+  return (1 + waves) * bias_len(max_distance) + 2 * n_buckets;
+}
+
+// A query whose every key the bias hides has lse2 = -inf; +inf in its place makes every
+// probability 2^(x - lse2) of the backward zero.
+template <bool BIAS> __device__ __forceinline__ float query_lse(float lse2) {
+  return BIAS && lse2 == -INFINITY ? INFINITY : lse2;
+}
+
+// Builds vec for head h (every thread of the workgroup; NTH threads; ends in a barrier).
+template <int NTH> __device__ __forceinline__ void bias_build(float* vec, const BiasArgs& a, int h, int H) {
+  int* bnd = reinterpret_cast<int*>(vec + bias_len(a.max_distance));
+  float* col = vec + bias_len(a.max_distance) + a.n_buckets;
+  for (int i = threadIdx.x; i < a.n_buckets; i += NTH) {
+    const float t = a.table[(int64_t)i * H + h];
+    bnd[i] = a.bounds[i];
+    col[i] = t <= BIAS_MASKED ? -INFINITY : t * LOG2E;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < bias_len(a.max_distance); i += NTH) {
+    const int n = min(max(i - BIAS_FRONT, 0), a.max_distance);
+    int lo = 0, hi = a.n_buckets;   // the last bucket whose bound is at or below n (bucket 0 if none)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (bnd[mid] <= n) lo = mid;
+      else hi = mid;
+    }
+    vec[i] = col[lo];
+  }
+  __syncthreads();
+}
+
+// Sums over the diagonals of dS. acc[i][r] of lane (g = l / 16, c = l % 16) holds the
+// sum over a block's tiles with qs - kt = i - 3 (query tile minus key tile) at distance
+// 16 (i - 3) + c - 4 g - r from the block's own. Moving the r-th value by r lanes within
+// the 16 lines the four up (what leaves a row at its start belongs to the window
+// before); the four lane groups then add into the wavefront's vector one after the
+// other, each to addresses of its own, so the order of the sums is fixed.
+// sums: entry of distance qw0 - k0 (the block's own).
+template <int NB> __device__ __forceinline__ void bias_add_diagonals(float* sums, const float (&acc)[NB][4]) {
+  const int l = lane_id(), g = l >> 4, c = l & 15;
+  float win[NB + 1];
+#pragma unroll
+  for (int i = -1; i < NB; ++i) {
+    float u = i >= 0 ? acc[i < 0 ? 0 : i][0] : 0.f;
+    if (i >= 0) {   // lane c takes lane c + r (row_shl)
+      const int k = i < 0 ? 0 : i;
+      u += dpp_shift<0x101>(acc[k][1]) + dpp_shift<0x102>(acc[k][2]) + dpp_shift<0x103>(acc[k][3]);
+    }
+    if (i + 1 < NB) {   // lane c takes lane c + r - 16 of the next window (row_shr 16 - r)
+      const int k = i + 1 < NB ? i + 1 : 0;
+      u += dpp_shift<0x11F>(acc[k][1]) + dpp_shift<0x11E>(acc[k][2]) + dpp_shift<0x11D>(acc[k][3]);
+    }
+    win[i + 1] = u;
+  }
+  float* at = sums + c - 4 * g;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (g == q) {
+#pragma unroll
+      for (int i = 0; i <= NB; ++i) lds_add(at + 16 * (i - 4), win[i]);
+    }
+    __builtin_amdgcn_wave_barrier();   // the four groups stay in this order
+  }
+}
+
+// The workgroup's sums by distance out to part (WAVES vectors behind one another;
+// far: each lane's sum over blocks beyond max_distance).
+template <int WAVES> __device__ __forceinline__ void bias_store_sums(float* sums, const BiasArgs& a, float far, float* out) {
+  const int len = bias_len(a.max_distance), w = threadIdx.x >> 6;
+  far = wave_sum(far);
+  if (lane_id() == 0) sums[w * len + BIAS_FRONT + a.max_distance] += far;
+  __syncthreads();
+  for (int n = threadIdx.x; n < a.max_distance; n += WAVES * 64) {
+    float s = 0.f;
+#pragma unroll
+    for (int u = 0; u < WAVES; ++u) s += sums[u * len + BIAS_FRONT + n];
+    out[n] = s;
+  }
+  if (w == 0) {   // max_distance and beyond
+    float s = 0.f;
+    for (int n = a.max_distance + lane_id(); n < a.max_distance + BIAS_TAIL; n += 64)
+#pragma unroll
+      for (int u = 0; u < WAVES; ++u) s += sums[u * len + BIAS_FRONT + n];
+    s = wave_sum(s);
+    if (lane_id() == 0) out[a.max_distance] = s;
+  }
+}
+
 // ---------------------------------------------------------------------------------------
-template <typename T, int DH, bool DROP>
-__global__ void __launch_bounds__(NT) attn_fwd_kernel(const T* qkv, T* out, float* lse2, int S, int H, int d,
-                                                       float scale_log2, DropArgs drop) {
+template <typename T, int DH, bool DROP, bool BIAS>
+__global__ void __launch_bounds__(NT) attn_fwd_kernel(QkvView<T> in, T* out, float* lse2, int S, int H, int d,
+                                                       float scale_log2, DropArgs drop, BiasArgs bias) {
+  extern __shared__ float bvec[];
   constexpr int V = Vec<T>::V;
   constexpr int BQ = 64;
   constexpr int DKV = DH / V;           // 16-byte vectors per head row
@@ -47,10 +170,9 @@ __global__ void __launch_bounds__(NT) attn_fwd_kernel(const T* qkv, T* out, floa
   const int qb = nqb - 1 - blockIdx.x;
   const int bh = blockIdx.y, b = bh / H, h = bh % H;
   const int w = threadIdx.x >> 6, l = lane_id();
-  const int64_t ld = 3 * (int64_t)d;
-  const T* Qp = qkv + (int64_t)b * S * ld + h * DH;
-  const T* Kp = Qp + d;
-  const T* Vp = Qp + 2 * d;
+  const T* Qp = in.q + (int64_t)b * S * in.ldq + h * DH;
+  const T* Kp = in.k + (int64_t)b * S * in.ldk + h * DH;
+  const T* Vp = in.v + (int64_t)b * S * in.ldv + h * DH;
   const int q0 = qb * BQ;
   const int qrow = q0 + 16 * w + (l & 15);
 
@@ -58,8 +180,9 @@ __global__ void __launch_bounds__(NT) attn_fwd_kernel(const T* qkv, T* out, floa
 #pragma unroll
   for (int s = 0; s < QSTEPS; ++s) {
     const int kv = s * 4 + (l >> 4);
-    qf[s] = (qrow < S) ? ld16(Qp + (int64_t)qrow * ld + kv * V) : u32x4{0, 0, 0, 0};
+    qf[s] = (qrow < S) ? ld16(Qp + (int64_t)qrow * in.ldq + kv * V) : u32x4{0, 0, 0, 0};
   }
+  if constexpr (BIAS) bias_build<NT>(bvec, bias, h, H);
   floatx4 acc[DH / 16];
 #pragma unroll
   for (int t = 0; t < DH / 16; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -69,8 +192,8 @@ __global__ void __launch_bounds__(NT) attn_fwd_kernel(const T* qkv, T* out, floa
   for (int kb = 0; kb <= last_kb; ++kb) {
     const int k0 = kb * BKV;
     __syncthreads();
-    stage_kmajor<T, BKV, DKV, NT>(sK, Kp + (int64_t)k0 * ld, (int)ld, S - k0);
-    stage_mnmajor<T, DH, BKV / V, NT>(sVt, Vp + (int64_t)k0 * ld, (int)ld, S - k0, typename AccPerm<T>::type());
+    stage_kmajor<T, BKV, DKV, NT>(sK, Kp + (int64_t)k0 * in.ldk, in.ldk, S - k0);
+    stage_mnmajor<T, DH, BKV / V, NT>(sVt, Vp + (int64_t)k0 * in.ldv, in.ldv, S - k0, typename AccPerm<T>::type());
     __syncthreads();
 
     floatx4 st[BKV / 16];
@@ -87,6 +210,7 @@ __global__ void __launch_bounds__(NT) attn_fwd_kernel(const T* qkv, T* out, floa
       for (int r = 0; r < 4; ++r) {
         const int key = k0 + kt * 16 + 4 * (l >> 4) + r;
         float x = st[kt][r] * scale_log2;
+        if constexpr (BIAS) x += bvec[BIAS_FRONT + min(max(qrow - key, 0), bias.max_distance)];
         if (key > qrow || key >= S) x = -INFINITY;
         st[kt][r] = x;
         mx = fmaxf(mx, x);
@@ -125,7 +249,7 @@ __global__ void __launch_bounds__(NT) attn_fwd_kernel(const T* qkv, T* out, floa
     }
   }
   if (qrow < S) {
-    const float inv = 1.f / l_run;
+    const float inv = BIAS && l_run == 0.f ? 0.f : 1.f / l_run;   // a bias of -inf can leave a query no key
     T* op = out + ((int64_t)b * S + qrow) * d + h * DH;
 #pragma unroll
     for (int t = 0; t < DH / 16; ++t) {
@@ -220,9 +344,10 @@ template <int DH, bool SMALL = false> struct FwdRing {
 // unit is not idle during the exponentials. A wavefront's queries start at a multiple of 16 * QS, which
 // divides 64, so every key block before its last one ends before its first
 // query and inside the sequence: only the last block is masked.
-template <int DH, bool DROP, bool SMALL>
-__global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_kernel(const bf16* qkv, bf16* out, float* lse2, int S, int H,
-                                                               int d, float scale_log2, DropArgs drop) {
+template <int DH, bool DROP, bool SMALL, bool BIAS>
+__global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_kernel(QkvView<bf16> in, bf16* out, float* lse2, int S, int H,
+                                                               int d, float scale_log2, DropArgs drop, BiasArgs bias) {
+  extern __shared__ float bvec[];
   using C = FwdRing<DH, SMALL>;
   constexpr int QS = C::QS, KS = C::KS, NS = C::NS, CPR = C::CPR;
   __shared__ u32x4 ring[NS * 2 * C::BLK];
@@ -231,10 +356,9 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   const int bh = blockIdx.x, b = bh / H, h = bh % H;
   const int w = threadIdx.x >> 6, l = lane_id(), g = l >> 4;
   const int wu = __builtin_amdgcn_readfirstlane(w);
-  const int64_t ld = 3 * (int64_t)d;
-  const bf16* Qp = qkv + (int64_t)b * S * ld + h * DH;
-  const bf16* Kp = Qp + d;
-  const bf16* Vp = Qp + 2 * d;
+  const bf16* Qp = in.q + (int64_t)b * S * in.ldq + h * DH;
+  const bf16* Kp = in.k + (int64_t)b * S * in.ldk + h * DH;
+  const bf16* Vp = in.v + (int64_t)b * S * in.ldv + h * DH;
   const int q0 = qb * C::BQ, qw0 = q0 + w * C::WQ;
   const uint32_t ring_lds = lds_addr(ring);
   const int nkb = min((q0 + C::BQ - 1) / BKV, (S - 1) / BKV) + 1;
@@ -246,12 +370,13 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
     const int row = qw0 + 16 * qs + (l & 15);
 #pragma unroll
     for (int s = 0; s < KS; ++s)
-      qf[qs][s] = (row < S) ? ld16(Qp + (int64_t)row * ld + s * 32 + 8 * g) : u32x4{0, 0, 0, 0};
+      qf[qs][s] = (row < S) ? ld16(Qp + (int64_t)row * in.ldq + s * 32 + 8 * g) : u32x4{0, 0, 0, 0};
   }
   floatx4 acc[QS][DH / 16];
   // the softmax normalizer: without dropout an MFMA of the probability
   // fragments against ones (the same bf16 P as the numerator, no cross-lane
-  // sums); with dropout a running sum of all of P in fp32
+  // sums); with dropout a running sum of all of P in fp32; with a bias, where the
+  // statistic is an output, each lane's own fp32 sum, joined at the end
   floatx4 lacc[QS];
   const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};   // bf16 1.0 pairs
   float m_run[QS], l_run[QS];
@@ -267,8 +392,8 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   auto fill = [&](int kb) {
     const uint32_t st = ring_lds + (uint32_t)((kb % NS) * 2 * C::BLK * 16);
     const int k0 = kb * BKV;
-    blk_fill<CPR, C::NTF>(Kp + (int64_t)k0 * ld, ld, S - k0, st, wu, l);
-    blk_fill<CPR, C::NTF>(Vp + (int64_t)k0 * ld, ld, S - k0, st + C::BLK * 16, wu, l);
+    blk_fill<CPR, C::NTF>(Kp + (int64_t)k0 * in.ldk, in.ldk, S - k0, st, wu, l);
+    blk_fill<CPR, C::NTF>(Vp + (int64_t)k0 * in.ldv, in.ldv, S - k0, st + C::BLK * 16, wu, l);
   };
   // raw scores q k^T of key block kb
   auto scores = [&](int kb, floatx4 (&sc)[QS][4]) {
@@ -290,9 +415,16 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   // accumulators, and the probabilities (dropped ones zeroed) as bf16 fragments
   auto softmax = [&](auto masked, int kb, floatx4 (&sc)[QS][4], u32x4 (&pf)[QS][2]) {
     const int k0 = kb * BKV;
+    const float* bp = BIAS ? bvec + BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) + (l & 15) - 4 * g : nullptr;
 #pragma unroll
     for (int qs = 0; qs < QS; ++qs) {
       const int qrow = qw0 + 16 * qs + (l & 15);
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[qs][kt][r] = fmaf(sc[qs][kt][r], scale_log2, bp[16 * (qs - kt) - r]);
+      }
       if constexpr (decltype(masked)::value) {
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
@@ -308,14 +440,22 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
 #pragma unroll
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[qs][kt][r]);
       mx = group4_max(mx);
-      const float m_new = fmaxf(m_run[qs], mx * scale_log2);
+      const float m_new = fmaxf(m_run[qs], BIAS ? mx : mx * scale_log2);
       const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
       const float alpha = fast_exp2(m_run[qs] - m_use);
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sc[qs][kt][r] = fast_exp2(fmaf(sc[qs][kt][r], scale_log2, -m_use));
-      if constexpr (DROP) {
+        for (int r = 0; r < 4; ++r)
+          sc[qs][kt][r] = fast_exp2(BIAS ? sc[qs][kt][r] - m_use : fmaf(sc[qs][kt][r], scale_log2, -m_use));
+      if constexpr (BIAS) {
+        float rs = 0.f;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) rs += sc[qs][kt][r];
+        l_run[qs] = l_run[qs] * alpha + rs;
+      } else if constexpr (DROP) {
         float rs = 0.f;
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
@@ -354,7 +494,7 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
 #pragma unroll
         for (int qs = 0; qs < QS; ++qs) mma_step<bf16>(acc[qs][t], vf, pf[qs][s]);
       }
-    if constexpr (!DROP) {
+    if constexpr (!DROP && !BIAS) {
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -403,6 +543,7 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   // compiler sees: it then knows qf has landed and puts no vmcnt(0) in the
   // loop, which would also wait for the ring's prefetches
   wait_vmcnt_all();
+  if constexpr (BIAS) bias_build<C::NTF>(bvec, bias, h, H);
   barrier_no_fence();
   if (PIPE && my_last >= 0) scores(0, sA);
   for (int kb = 0; kb < nkb; kb += 2) {
@@ -413,8 +554,9 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   for (int qs = 0; qs < QS; ++qs) {
     const int qrow = qw0 + 16 * qs + (l & 15);
     if (qrow < S) {
-      if constexpr (!DROP) l_run[qs] = lacc[qs][0];   // every row of the product holds the row sum
-      const float inv = 1.f / l_run[qs];
+      if constexpr (BIAS) l_run[qs] = group4_sum(l_run[qs]);
+      else if constexpr (!DROP) l_run[qs] = lacc[qs][0];   // every row of the product holds the row sum
+      const float inv = BIAS && l_run[qs] == 0.f ? 0.f : 1.f / l_run[qs];   // a bias of -inf can leave a query no key
       bf16* op = out + ((int64_t)b * S + qrow) * d + h * DH;
 #pragma unroll
       for (int t = 0; t < DH / 16; ++t)
@@ -455,10 +597,11 @@ __global__ void __launch_bounds__(NT) attn_dsum_kernel(const T* o, const T* dO, 
 }
 
 // ---------------------------------------------------------------------------------------
-template <typename T, int DH, bool DROP>
-__global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(const T* qkv, const T* dO, const float* lse2,
-                                                            const float* Dsum, T* dqkv, int S, int H, int d,
-                                                            float scale_log2, float scale, DropArgs drop) {
+template <typename T, int DH, bool DROP, bool BIAS>
+__global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(QkvView<T> in, const T* dO, const float* lse2,
+                                                            const float* Dsum, GradView<T> grad, int S, int H, int d,
+                                                            float scale_log2, float scale, DropArgs drop, BiasArgs bias) {
+  extern __shared__ float bvec[];
   constexpr int V = Vec<T>::V;
   constexpr int BQ = (DH >= 128) ? 32 : 64;  // queries per staged block (LDS budget)
   constexpr int DKV = DH / V;
@@ -473,10 +616,9 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(const T* qkv, const T
   const int kb = blockIdx.x;
   const int bh = blockIdx.y, b = bh / H, h = bh % H;
   const int w = threadIdx.x >> 6, l = lane_id();
-  const int64_t ld = 3 * (int64_t)d;
-  const T* Qp = qkv + (int64_t)b * S * ld + h * DH;
-  const T* Kp = Qp + d;
-  const T* Vp = Qp + 2 * d;
+  const T* Qp = in.q + (int64_t)b * S * in.ldq + h * DH;
+  const T* Kp = in.k + (int64_t)b * S * in.ldk + h * DH;
+  const T* Vp = in.v + (int64_t)b * S * in.ldv + h * DH;
   const T* dOp = dO + (int64_t)b * S * d + h * DH;
   const float* Lp = lse2 + (int64_t)bh * S;
   const float* Dp = Dsum + (int64_t)bh * S;
@@ -487,22 +629,23 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(const T* qkv, const T
 #pragma unroll
   for (int s = 0; s < QSTEPS; ++s) {
     const int kv = s * 4 + (l >> 4);
-    kf[s] = (key < S) ? ld16(Kp + (int64_t)key * ld + kv * V) : u32x4{0, 0, 0, 0};
-    vf[s] = (key < S) ? ld16(Vp + (int64_t)key * ld + kv * V) : u32x4{0, 0, 0, 0};
+    kf[s] = (key < S) ? ld16(Kp + (int64_t)key * in.ldk + kv * V) : u32x4{0, 0, 0, 0};
+    vf[s] = (key < S) ? ld16(Vp + (int64_t)key * in.ldv + kv * V) : u32x4{0, 0, 0, 0};
   }
+  if constexpr (BIAS) bias_build<NT>(bvec, bias, h, H);
   floatx4 adk[DH / 16], adv[DH / 16];
 #pragma unroll
   for (int t = 0; t < DH / 16; ++t) adk[t] = adv[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
   for (int q0 = (k0 / BQ) * BQ; q0 < S; q0 += BQ) {
     __syncthreads();
-    stage_kmajor<T, BQ, DKV, NT>(sQ, Qp + (int64_t)q0 * ld, (int)ld, S - q0);
+    stage_kmajor<T, BQ, DKV, NT>(sQ, Qp + (int64_t)q0 * in.ldq, in.ldq, S - q0);
     stage_kmajor<T, BQ, DKV, NT>(sdO, dOp + (int64_t)q0 * d, d, S - q0);
-    stage_mnmajor<T, DH, BQ / V, NT>(sQt, Qp + (int64_t)q0 * ld, (int)ld, S - q0, typename AccPerm<T>::type());
+    stage_mnmajor<T, DH, BQ / V, NT>(sQt, Qp + (int64_t)q0 * in.ldq, in.ldq, S - q0, typename AccPerm<T>::type());
     stage_mnmajor<T, DH, BQ / V, NT>(sdOt, dOp + (int64_t)q0 * d, d, S - q0, typename AccPerm<T>::type());
     if (threadIdx.x < BQ) {
       const int q = q0 + threadIdx.x;
-      sL[threadIdx.x] = (q < S) ? Lp[q] : 0.f;
+      sL[threadIdx.x] = (q < S) ? query_lse<BIAS>(Lp[q]) : 0.f;
       sD[threadIdx.x] = (q < S) ? Dp[q] : 0.f;
     }
     __syncthreads();
@@ -521,7 +664,8 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(const T* qkv, const T
         const int qi = qt * 16 + 4 * (l >> 4) + r;
         const int q = q0 + qi;
         const bool ok = (key <= q) && (q < S) && (key < S);
-        const float p = ok ? exp2f(s[r] * scale_log2 - sL[qi]) : 0.f;
+        const float bv = BIAS ? bvec[BIAS_FRONT + min(max(q - key, 0), bias.max_distance)] : 0.f;
+        const float p = ok ? exp2f((BIAS ? s[r] * scale_log2 + bv : s[r] * scale_log2) - sL[qi]) : 0.f;
         // dropout M = keep * scale: dV takes P M, dP = (dO V^T) M
         const float mk = DROP ? (((bits >> r) & 1) ? drop.scale : 0.f) : 1.f;
         P[qt][r] = p * mk;
@@ -539,8 +683,8 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(const T* qkv, const T
     }
   }
   if (key < S) {
-    T* dk = dqkv + ((int64_t)b * S + key) * ld + d + h * DH;
-    T* dv = dk + d;
+    T* dk = grad.k + ((int64_t)b * S + key) * grad.ldk + h * DH;
+    T* dv = grad.v + ((int64_t)b * S + key) * grad.ldv + h * DH;
 #pragma unroll
     for (int t = 0; t < DH / 16; ++t) {
       const int c = t * 16 + 4 * (l >> 4);
@@ -553,10 +697,11 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(const T* qkv, const T
   }
 }
 
-template <typename T, int DH, bool DROP>
-__global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(const T* qkv, const T* dO, const float* lse2,
-                                                          const float* Dsum, T* dqkv, int S, int H, int d,
-                                                          float scale_log2, float scale, DropArgs drop) {
+template <typename T, int DH, bool DROP, bool BIAS>
+__global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(QkvView<T> in, const T* dO, const float* lse2,
+                                                          const float* Dsum, GradView<T> grad, int S, int H, int d,
+                                                          float scale_log2, float scale, DropArgs drop, BiasArgs bias) {
+  extern __shared__ float bvec[];
   constexpr int V = Vec<T>::V;
   constexpr int BQ = 64;
   constexpr int DKV = DH / V;
@@ -570,23 +715,29 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(const T* qkv, const T* 
   const int qb = nqb - 1 - blockIdx.x;
   const int bh = blockIdx.y, b = bh / H, h = bh % H;
   const int w = threadIdx.x >> 6, l = lane_id();
-  const int64_t ld = 3 * (int64_t)d;
-  const T* Qp = qkv + (int64_t)b * S * ld + h * DH;
-  const T* Kp = Qp + d;
-  const T* Vp = Qp + 2 * d;
+  const T* Qp = in.q + (int64_t)b * S * in.ldq + h * DH;
+  const T* Kp = in.k + (int64_t)b * S * in.ldk + h * DH;
+  const T* Vp = in.v + (int64_t)b * S * in.ldv + h * DH;
   const T* dOp = dO + (int64_t)b * S * d + h * DH;
   const int q0 = qb * BQ;
   const int qrow = q0 + 16 * w + (l & 15);
   const bool qok = qrow < S;
-  const float lq = qok ? lse2[(int64_t)bh * S + qrow] : 0.f;
+  const float lq = qok ? query_lse<BIAS>(lse2[(int64_t)bh * S + qrow]) : 0.f;
   const float Dq = qok ? Dsum[(int64_t)bh * S + qrow] : 0.f;
 
   u32x4 qf[QSTEPS], gf[QSTEPS];
 #pragma unroll
   for (int s = 0; s < QSTEPS; ++s) {
     const int kv = s * 4 + (l >> 4);
-    qf[s] = qok ? ld16(Qp + (int64_t)qrow * ld + kv * V) : u32x4{0, 0, 0, 0};
+    qf[s] = qok ? ld16(Qp + (int64_t)qrow * in.ldq + kv * V) : u32x4{0, 0, 0, 0};
     gf[s] = qok ? ld16(dOp + (int64_t)qrow * d + kv * V) : u32x4{0, 0, 0, 0};
+  }
+  float* sums = nullptr;   // this wavefront's sums of dS by distance
+  if constexpr (BIAS) {
+    sums = bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets;
+    for (int i = threadIdx.x; i < (NT / 64) * bias_len(bias.max_distance); i += NT) sums[i] = 0.f;
+    sums += w * bias_len(bias.max_distance);
+    bias_build<NT>(bvec, bias, h, H);
   }
   floatx4 adq[DH / 16];
 #pragma unroll
@@ -596,9 +747,9 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(const T* qkv, const T* 
   for (int kb = 0; kb <= last_kb; ++kb) {
     const int k0 = kb * BKV;
     __syncthreads();
-    stage_kmajor<T, BKV, DKV, NT>(sK, Kp + (int64_t)k0 * ld, (int)ld, S - k0);
-    stage_kmajor<T, BKV, DKV, NT>(sV, Vp + (int64_t)k0 * ld, (int)ld, S - k0);
-    stage_mnmajor<T, DH, BKV / V, NT>(sKt, Kp + (int64_t)k0 * ld, (int)ld, S - k0, typename AccPerm<T>::type());
+    stage_kmajor<T, BKV, DKV, NT>(sK, Kp + (int64_t)k0 * in.ldk, in.ldk, S - k0);
+    stage_kmajor<T, BKV, DKV, NT>(sV, Vp + (int64_t)k0 * in.ldv, in.ldv, S - k0);
+    stage_mnmajor<T, DH, BKV / V, NT>(sKt, Kp + (int64_t)k0 * in.ldk, in.ldk, S - k0, typename AccPerm<T>::type());
     __syncthreads();
     floatx4 dS[BKV / 16];
 #pragma unroll
@@ -614,9 +765,20 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(const T* qkv, const T* 
       for (int r = 0; r < 4; ++r) {
         const int key = k0 + kt * 16 + 4 * (l >> 4) + r;
         const bool ok = qok && (key <= qrow) && (key < S);
-        const float p = ok ? exp2f(s[r] * scale_log2 - lq) : 0.f;
+        const float bv = BIAS ? bvec[BIAS_FRONT + min(max(qrow - key, 0), bias.max_distance)] : 0.f;
+        const float p = ok ? exp2f((BIAS ? s[r] * scale_log2 + bv : s[r] * scale_log2) - lq) : 0.f;
         const float mk = DROP ? (((bits >> r) & 1) ? drop.scale : 0.f) : 1.f;
         dS[kt][r] = p * (dp[r] * mk - Dq);
+      }
+    }
+    if constexpr (BIAS) {
+      if (bias.part != nullptr) {   // uniform
+        float acc[4][4];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[3 - kt][r] = dS[kt][r];
+        bias_add_diagonals<4>(sums + BIAS_FRONT + min(q0 + 16 * w - k0, bias.max_distance + 63), acc);
       }
     }
 #pragma unroll
@@ -627,13 +789,18 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(const T* qkv, const T* 
     }
   }
   if (qok) {
-    T* dq = dqkv + ((int64_t)b * S + qrow) * ld + h * DH;
+    T* dq = grad.q + ((int64_t)b * S + qrow) * grad.ldq + h * DH;
 #pragma unroll
     for (int t = 0; t < DH / 16; ++t) {
       const int c = t * 16 + 4 * (l >> 4);
 #pragma unroll
       for (int r = 0; r < 4; ++r) dq[c + r] = from_f32<T>(adq[t][r] * scale);
     }
+  }
+  if constexpr (BIAS) {
+    if (bias.part != nullptr)
+      bias_store_sums<NT / 64>(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets, bias, 0.f,
+                               bias.part + ((int64_t)bh * nqb + qb) * (bias.max_distance + 1));
   }
 }
 
@@ -673,7 +840,7 @@ template <int DH, bool SMALL = false> struct BwdRing {
 constexpr int PAIR_ROWS = 2;
 template <int DH>
 __global__ void __launch_bounds__(NT) attn_pairs_kernel(const bf16* o, const bf16* dO, const float* lse2, float* pairs,
-                                                         int S, int S_pad, int H, int d, int64_t rows) {
+                                                         int S, int S_pad, int H, int d, int64_t rows, bool bias) {
   constexpr int LPR = DH / 8;
   const int64_t gid = (int64_t)blockIdx.x * NT + threadIdx.x;
   const int64_t row0 = gid / LPR * PAIR_ROWS;  // row = token * H + h
@@ -697,7 +864,8 @@ __global__ void __launch_bounds__(NT) attn_pairs_kernel(const bf16* o, const bf1
     if (row < rows && part == 0) {
       const int64_t tok = row / H, bq = tok / S, q = tok % S;
       const int64_t bh = bq * H + row % H;
-      pairs[(bh * S_pad + q) * 2] = lse2[bh * S + q];
+      const float lq = lse2[bh * S + q];
+      pairs[(bh * S_pad + q) * 2] = bias ? query_lse<true>(lq) : lq;
       pairs[(bh * S_pad + q) * 2 + 1] = sum;
     }
   }
@@ -715,9 +883,9 @@ __global__ void __launch_bounds__(NT) attn_pairs_kernel(const bf16* o, const bf1
 // the qkv projection: lane l holds columns 4 (l >> 4) + r of 16-column tile t,
 // for token l & 15; the 16 lanes of equal l >> 4 (one DPP row) are summed with
 // row moves, the waves through LDS (red: WAVES * NCOL floats, free for this
-// use), and each column goes out as one atomic add to gbias[col(c)].
+// use), and each column goes out as one atomic add to col(c), unless that is null.
 template <int WAVES, int NCOL, class Col>
-__device__ __forceinline__ void colsum_tiles(float (&v)[NCOL / 16][4], float* red, float* gbias, Col col) {
+__device__ __forceinline__ void colsum_tiles(float (&v)[NCOL / 16][4], float* red, Col col) {
   const int w = threadIdx.x >> 6, l = lane_id(), g = l >> 4;
 #pragma unroll
   for (int t = 0; t < NCOL / 16; ++t)
@@ -734,25 +902,26 @@ __device__ __forceinline__ void colsum_tiles(float (&v)[NCOL / 16][4], float* re
     float sum = 0.f;
 #pragma unroll
     for (int u = 0; u < WAVES; ++u) sum += red[u * NCOL + c];
-    atomicAdd(gbias + col(c), sum);
+    float* to = col(c);
+    if (to != nullptr) atomicAdd(to, sum);
   }
 }
 
 // dK/dV of key block kb (ring: NS * STAGE slots of LDS)
-template <int DH, bool DROP, bool SMALL>
-__device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* qkv, const bf16* dO,
-                                               const float* pairs, bf16* dqkv, int S, int S_pad, int H, int d,
-                                               float scale_log2, float scale, float* gbias, const DropArgs& drop) {
+template <int DH, bool DROP, bool SMALL, bool BIAS>
+__device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb, const QkvView<bf16>& in, const bf16* dO,
+                                               const float* pairs, const GradView<bf16>& grad, int S, int S_pad, int H,
+                                               int d, float scale_log2, float scale, const DropArgs& drop,
+                                               const BiasArgs& bias) {
   using C = BwdRing<DH, SMALL>;
   constexpr int SUB = C::SUB, KST = C::KST, NS = C::NS, CPR = C::CPR;
   static_assert(NS * C::STAGE * 4 >= C::WAVES * 2 * DH, "LDS for the column sums");
   const int bh = blockIdx.x, b = bh / H, h = bh % H;
   const int w = threadIdx.x >> 6, l = lane_id(), g = l >> 4;
   const int wu = __builtin_amdgcn_readfirstlane(w);
-  const int64_t ld = 3 * (int64_t)d;
-  const bf16* Qp = qkv + (int64_t)b * S * ld + h * DH;
-  const bf16* Kp = Qp + d;
-  const bf16* Vp = Qp + 2 * d;
+  const bf16* Qp = in.q + (int64_t)b * S * in.ldq + h * DH;
+  const bf16* Kp = in.k + (int64_t)b * S * in.ldk + h * DH;
+  const bf16* Vp = in.v + (int64_t)b * S * in.ldv + h * DH;
   const bf16* dOp = dO + (int64_t)b * S * d + h * DH;
   const float* Pp = pairs + (int64_t)bh * S_pad * 2;
   const uint32_t ring_lds = lds_addr(ring);
@@ -766,8 +935,8 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* 
     const int key = kw0 + 16 * ks + (l & 15);
 #pragma unroll
     for (int st = 0; st < KST; ++st) {
-      kf[ks][st] = (key < S) ? ld16(Kp + (int64_t)key * ld + st * 32 + 8 * g) : u32x4{0, 0, 0, 0};
-      vf[ks][st] = (key < S) ? ld16(Vp + (int64_t)key * ld + st * 32 + 8 * g) : u32x4{0, 0, 0, 0};
+      kf[ks][st] = (key < S) ? ld16(Kp + (int64_t)key * in.ldk + st * 32 + 8 * g) : u32x4{0, 0, 0, 0};
+      vf[ks][st] = (key < S) ? ld16(Vp + (int64_t)key * in.ldv + st * 32 + 8 * g) : u32x4{0, 0, 0, 0};
     }
   }
   floatx4 adk[SUB][DH / 16], adv[SUB][DH / 16];
@@ -779,7 +948,7 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* 
   auto fill = [&](int j) {
     const uint32_t st = ring_lds + (uint32_t)((j % NS) * C::STAGE * 16);
     const int q0 = (qb_first + j) * 64;
-    blk_fill<CPR, C::NTB>(Qp + (int64_t)q0 * ld, ld, S - q0, st, wu, l);
+    blk_fill<CPR, C::NTB>(Qp + (int64_t)q0 * in.ldq, in.ldq, S - q0, st, wu, l);
     blk_fill<CPR, C::NTB>(dOp + (int64_t)q0 * d, d, S - q0, st + C::BLK * 16, wu, l);
     if (wu == 0 && l < C::PAIR_SLOTS) dma16(Pp + (int64_t)q0 * 2 + l * 4, st + 2 * C::BLK * 16);
   };
@@ -787,6 +956,7 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* 
   for (int t = 0; t < NS - 1; ++t)
     if (t < njobs) fill(t);
   wait_vmcnt_all();   // kf and vf known complete: no vmcnt(0) inside the loop
+  if constexpr (BIAS) bias_build<C::NTB>(bvec, bias, h, H);
   for (int j = 0; j < njobs; ++j) {
     wait_loads<C::L, NS - 2>(min(njobs - 1, j + NS - 2) - j);
     wait_lds_reads();
@@ -799,6 +969,8 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* 
     const float* sP = reinterpret_cast<const float*>(sQ + 2 * C::BLK);
     const int q0 = qb * 64;
     const bool edge = (q0 < kw0 + C::WR - 1) || (q0 + 64 > S) || (kw0 + C::WR > S);
+    // the bias of query 16 t + 4 g + r and key 16 ks + l % 16 of these: bp[16 (t - ks) + r]
+    const float* bp = BIAS ? bvec + BIAS_FRONT + min(q0 - kw0, bias.max_distance + C::WR - 1) + 4 * g - (l & 15) : nullptr;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {   // 32 queries: tiles 2s and 2s + 1
       floatx4 sc[SUB][2], dp[SUB][2];
@@ -833,7 +1005,8 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* 
             const float lq = sP[2 * qi], Dq = sP[2 * qi + 1];
 #pragma unroll
             for (int ks = 0; ks < SUB; ++ks) {
-              float x = fmaf(sc[ks][u][r], scale_log2, -lq);
+              float x = BIAS ? fmaf(sc[ks][u][r], scale_log2, bp[16 * (2 * s + u - ks) + r]) - lq
+                             : fmaf(sc[ks][u][r], scale_log2, -lq);
               if constexpr (decltype(masked)::value) {
                 const int key = kw0 + 16 * ks + (l & 15);
                 x = (key <= q0 + qi && q0 + qi < S && key < S) ? x : -INFINITY;
@@ -873,8 +1046,8 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* 
   for (int ks = 0; ks < SUB; ++ks) {
     const int key = kw0 + 16 * ks + (l & 15);
     if (key < S) {
-      bf16* dk = dqkv + ((int64_t)b * S + key) * ld + d + h * DH;
-      bf16* dv = dk + d;
+      bf16* dk = grad.k + ((int64_t)b * S + key) * grad.ldk + h * DH;
+      bf16* dv = grad.v + ((int64_t)b * S + key) * grad.ldv + h * DH;
 #pragma unroll
       for (int t = 0; t < DH / 16; ++t) {
         *reinterpret_cast<u32x2*>(dk + t * 16 + 4 * g) =
@@ -885,7 +1058,7 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* 
       }
     }
   }
-  if (gbias != nullptr) {   // uniform: G_bqkv += column sums of dK and dV over this workgroup's keys
+  if (grad.sv != nullptr) {   // uniform: bias gradients += column sums of dK and dV over this workgroup's keys
     float v[2 * DH / 16][4];
 #pragma unroll
     for (int t = 0; t < DH / 16; ++t)
@@ -901,16 +1074,18 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, int kb, const bf16* 
         v[DH / 16 + t][r] = sv;
       }
     __syncthreads();   // every wave is done with the ring
-    colsum_tiles<C::WAVES, 2 * DH>(v, reinterpret_cast<float*>(ring), gbias,
-                                   [&](int c) { return (c < DH ? d : 2 * d - DH) + h * DH + c; });
+    colsum_tiles<C::WAVES, 2 * DH>(v, reinterpret_cast<float*>(ring), [&](int c) -> float* {
+      return c >= DH ? grad.sv + h * DH + c - DH : grad.sk != nullptr ? grad.sk + h * DH + c : nullptr;
+    });
   }
 }
 
 // dQ of query block nqb - 1 - yb (ring: NS * 2 * BLK slots of LDS)
-template <int DH, bool DROP, bool SMALL>
-__device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qkv, const bf16* dO,
-                                             const float* pairs, bf16* dqkv, int S, int S_pad, int H, int d,
-                                             float scale_log2, float scale, float* gbias, const DropArgs& drop) {
+template <int DH, bool DROP, bool SMALL, bool BIAS>
+__device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, const QkvView<bf16>& in, const bf16* dO,
+                                             const float* pairs, const GradView<bf16>& grad, int S, int S_pad, int H,
+                                             int d, float scale_log2, float scale, const DropArgs& drop,
+                                             const BiasArgs& bias) {
   using C = BwdRing<DH, SMALL>;
   constexpr int SUB = C::SUB, KST = C::KST, NS = C::NS, CPR = C::CPR;
   static_assert(NS * 2 * C::BLK * 4 >= C::WAVES * DH, "LDS for the column sums");
@@ -919,10 +1094,9 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
   const int bh = blockIdx.x, b = bh / H, h = bh % H;
   const int w = threadIdx.x >> 6, l = lane_id(), g = l >> 4;
   const int wu = __builtin_amdgcn_readfirstlane(w);
-  const int64_t ld = 3 * (int64_t)d;
-  const bf16* Qp = qkv + (int64_t)b * S * ld + h * DH;
-  const bf16* Kp = Qp + d;
-  const bf16* Vp = Qp + 2 * d;
+  const bf16* Qp = in.q + (int64_t)b * S * in.ldq + h * DH;
+  const bf16* Kp = in.k + (int64_t)b * S * in.ldk + h * DH;
+  const bf16* Vp = in.v + (int64_t)b * S * in.ldv + h * DH;
   const bf16* dOp = dO + (int64_t)b * S * d + h * DH;
   const float* Pp = pairs + (int64_t)bh * S_pad * 2;
   const uint32_t ring_lds = lds_addr(ring);
@@ -938,7 +1112,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
     const bool ok = q < S;
 #pragma unroll
     for (int st = 0; st < KST; ++st) {
-      qf[qs][st] = ok ? ld16(Qp + (int64_t)q * ld + st * 32 + 8 * g) : u32x4{0, 0, 0, 0};
+      qf[qs][st] = ok ? ld16(Qp + (int64_t)q * in.ldq + st * 32 + 8 * g) : u32x4{0, 0, 0, 0};
       gf[qs][st] = ok ? ld16(dOp + (int64_t)q * d + st * 32 + 8 * g) : u32x4{0, 0, 0, 0};
     }
     lq[qs] = ok ? Pp[2 * q] : 0.f;
@@ -953,13 +1127,20 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
   auto fill = [&](int kb) {
     const uint32_t st = ring_lds + (uint32_t)((kb % NS) * 2 * C::BLK * 16);
     const int k0 = kb * BKV;
-    blk_fill<CPR, C::NTB>(Kp + (int64_t)k0 * ld, ld, S - k0, st, wu, l);
-    blk_fill<CPR, C::NTB>(Vp + (int64_t)k0 * ld, ld, S - k0, st + C::BLK * 16, wu, l);
+    blk_fill<CPR, C::NTB>(Kp + (int64_t)k0 * in.ldk, in.ldk, S - k0, st, wu, l);
+    blk_fill<CPR, C::NTB>(Vp + (int64_t)k0 * in.ldv, in.ldv, S - k0, st + C::BLK * 16, wu, l);
   };
 #pragma unroll
   for (int t = 0; t < NS - 1; ++t)
     if (t < nkb) fill(t);
   wait_vmcnt_all();   // qf, gf, lq and Dq known complete: no vmcnt(0) inside the loop
+  float* sums = nullptr;   // this wavefront's sums of dS by distance
+  if constexpr (BIAS) {
+    sums = bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets;
+    for (int i = threadIdx.x; i < C::WAVES * bias_len(bias.max_distance); i += C::NTB) sums[i] = 0.f;
+    sums += w * bias_len(bias.max_distance);
+    bias_build<C::NTB>(bvec, bias, h, H);
+  }
   for (int kb = 0; kb < nkb; ++kb) {
     wait_loads<C::L, NS - 2>(min(nkb - 1, kb + NS - 2) - kb);
     wait_lds_reads();
@@ -970,6 +1151,15 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
     const u32x4* sV = sK + C::BLK;
     const int k0 = kb * BKV;
     const bool edge = (k0 + BKV - 1 > qw0) || (k0 + BKV > S) || (qw0 + C::WR > S);
+    const int dist = BIAS ? BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) : 0;   // entry of the block's own distance
+    const float* bp = BIAS ? bvec + dist + (l & 15) - 4 * g : nullptr;
+    float diag[SUB + 3][4];
+    if constexpr (BIAS) {
+#pragma unroll
+      for (int i = 0; i < SUB + 3; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) diag[i][r] = 0.f;
+    }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {   // 32 keys: tiles 2s and 2s + 1
       floatx4 sc[SUB][2], dp[SUB][2];
@@ -1002,7 +1192,8 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
             const uint32_t bits = dbits[u];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float x = fmaf(sc[qs][u][r], scale_log2, -lq[qs]);
+              float x = BIAS ? fmaf(sc[qs][u][r], scale_log2, bp[16 * (qs - 2 * s - u) - r]) - lq[qs]
+                             : fmaf(sc[qs][u][r], scale_log2, -lq[qs]);
               if constexpr (decltype(masked)::value) {
                 const int key = k0 + (2 * s + u) * 16 + 4 * g + r;
                 x = (key <= q && key < S && q < S) ? x : -INFINITY;
@@ -1010,6 +1201,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
               const float p = fast_exp2(x);
               const float mk = DROP ? (((bits >> r) & 1) ? drop.scale : 0.f) : 1.f;
               dp[qs][u][r] = p * (dp[qs][u][r] * mk - Dq[qs]);
+              if constexpr (BIAS) diag[qs - 2 * s - u + 3][r] += dp[qs][u][r];
             }
           }
         }
@@ -1026,12 +1218,15 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
         for (int qs = 0; qs < SUB; ++qs) mma_step<bf16>(adq[qs][t], kt, dsf[qs]);
       }
     }
+    if constexpr (BIAS) {
+      if (bias.part != nullptr) bias_add_diagonals<SUB + 3>(sums + dist, diag);
+    }
   }
 #pragma unroll
   for (int qs = 0; qs < SUB; ++qs) {
     const int q = qw0 + 16 * qs + (l & 15);
     if (q < S) {
-      bf16* dq = dqkv + ((int64_t)b * S + q) * ld + h * DH;
+      bf16* dq = grad.q + ((int64_t)b * S + q) * grad.ldq + h * DH;
 #pragma unroll
       for (int t = 0; t < DH / 16; ++t)
         *reinterpret_cast<u32x2*>(dq + t * 16 + 4 * g) =
@@ -1039,7 +1234,12 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
                   pack_bf16x2(adq[qs][t][2] * scale, adq[qs][t][3] * scale)};
     }
   }
-  if (gbias != nullptr) {   // uniform: G_bqkv += column sums of dQ over this workgroup's queries
+  if constexpr (BIAS) {
+    if (bias.part != nullptr)
+      bias_store_sums<C::WAVES>(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets, bias, 0.f,
+                                bias.part + ((int64_t)bh * nqb + qb) * (bias.max_distance + 1));
+  }
+  if (grad.sq != nullptr) {   // uniform: bias gradient += column sums of dQ over this workgroup's queries
     float v[DH / 16][4];
 #pragma unroll
     for (int t = 0; t < DH / 16; ++t)
@@ -1051,7 +1251,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
         v[t][r] = sq * scale;
       }
     __syncthreads();   // every wave is done with the ring
-    colsum_tiles<C::WAVES, DH>(v, reinterpret_cast<float*>(ring), gbias, [&](int c) { return h * DH + c; });
+    colsum_tiles<C::WAVES, DH>(v, reinterpret_cast<float*>(ring), [&](int c) { return grad.sq + h * DH + c; });
   }
 }
 
@@ -1059,19 +1259,57 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, int yb, const bf16* qk
 // block y, smallest keys first; the rest: dQ, largest queries first), so that
 // the tail of the dK/dV blocks overlaps the first dQ blocks and the two share
 // CUs (7% faster than two launches at head dim 64).
-template <int DH, bool DROP, bool SMALL>
-__global__ void __launch_bounds__((BwdRing<DH, SMALL>::NTB), (BwdRing<DH, SMALL>::OCC)) attn_bwd_ring_kernel(const bf16* qkv, const bf16* dO, const float* pairs,
-                                                               bf16* dqkv, int S, int S_pad, int H, int d,
-                                                               float scale_log2, float scale, float* gbias,
-                                                               DropArgs drop, int ny) {
+template <int DH, bool DROP, bool SMALL, bool BIAS>
+__global__ void __launch_bounds__((BwdRing<DH, SMALL>::NTB), (BwdRing<DH, SMALL>::OCC)) attn_bwd_ring_kernel(QkvView<bf16> in, const bf16* dO, const float* pairs,
+                                                               GradView<bf16> grad, int S, int S_pad, int H, int d,
+                                                               float scale_log2, float scale, DropArgs drop, int ny,
+                                                               BiasArgs bias) {
   using C = BwdRing<DH, SMALL>;
   constexpr int SLOTS = C::STAGE > 2 * C::BLK ? C::NS * C::STAGE : C::NS * 2 * C::BLK;
   __shared__ u32x4 ring[SLOTS];
+  extern __shared__ float bvec[];
   if ((int)blockIdx.y < ny)
-    dkdv_ring_body<DH, DROP, SMALL>(ring, blockIdx.y, qkv, dO, pairs, dqkv, S, S_pad, H, d, scale_log2, scale, gbias, drop);
+    dkdv_ring_body<DH, DROP, SMALL, BIAS>(ring, bvec, blockIdx.y, in, dO, pairs, grad, S, S_pad, H, d, scale_log2, scale, drop,
+                                          bias);
   else
-    dq_ring_body<DH, DROP, SMALL>(ring, blockIdx.y - ny, qkv, dO, pairs, dqkv, S, S_pad, H, d, scale_log2, scale, gbias,
-                           drop);
+    dq_ring_body<DH, DROP, SMALL, BIAS>(ring, bvec, blockIdx.y - ny, in, dO, pairs, grad, S, S_pad, H, d, scale_log2, scale,
+                                        drop, bias);
+}
+
+// g_table[bucket][h] += sum over the rows (sequences and query blocks) of head h of
+// part [rows][n = max_distance + 1], by bucket. One workgroup per head: the rows are
+// summed per distance (a fixed number of row groups, each in order), then a wavefront
+// sums the distances of a bucket.
+constexpr int BS_NT = 1024;
+__global__ void __launch_bounds__(BS_NT) attn_bias_sums_kernel(const float* __restrict__ part, int batch, int blocks, int H,
+                                                               const int32_t* __restrict__ bounds, int n_buckets,
+                                                               int max_distance, float* g_table) {
+  __shared__ float red[BS_NT];
+  __shared__ float dist[MAX_DISTANCE + 1];
+  const int h = blockIdx.x, n = max_distance + 1, rows = batch * blocks;
+  const int cl = threadIdx.x & 63, rg = threadIdx.x >> 6;   // 64 distances x 16 row groups
+  for (int n0 = 0; n0 < n; n0 += 64) {
+    float s = 0.f;
+    if (n0 + cl < n) {
+#pragma unroll 4
+      for (int r = rg; r < rows; r += BS_NT / 64)
+        s += part[(((int64_t)(r / blocks) * H + h) * blocks + r % blocks) * n + n0 + cl];
+    }
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (rg == 0 && n0 + cl < n) {
+      for (int q = 1; q < BS_NT / 64; ++q) s += red[q * 64 + cl];
+      dist[n0 + cl] = s;
+    }
+    __syncthreads();
+  }
+  for (int b = rg; b < n_buckets; b += BS_NT / 64) {
+    const int lo = b == 0 ? 0 : max(bounds[b], 0), hi = b + 1 < n_buckets ? min(bounds[b + 1], n) : n;
+    float s = 0.f;
+    for (int i = lo + cl; i < hi; i += 64) s += dist[i];
+    s = wave_sum(s);
+    if (cl == 0) g_table[(int64_t)b * H + h] += s;
+  }
 }
 
 // Whether workgroups of 64 rows (SMALL) fit the CUs about twice, so that the
@@ -1080,132 +1318,164 @@ __global__ void __launch_bounds__((BwdRing<DH, SMALL>::NTB), (BwdRing<DH, SMALL>
 // between more rows.
 bool small_grid(int64_t heads, int S) { return heads * ((S + 63) / 64) <= 2 * cu_count(); }
 
+template <typename T> QkvView<T> view(const AttnArgs& a) {
+  return {reinterpret_cast<const T*>(a.q), reinterpret_cast<const T*>(a.k), reinterpret_cast<const T*>(a.v), a.ldq, a.ldk,
+          a.ldv};
+}
+BiasArgs bias_args(const AttnArgs& a) { return {a.table, a.bounds, a.n_buckets, a.max_distance, nullptr}; }
+// bytes of LDS behind the tiles
+size_t bias_lds(const AttnArgs& a, int waves) {
+  return a.table ? sizeof(float) * (size_t)bias_lds_floats(a.max_distance, a.n_buckets, waves) : 0;
+}
+
 template <typename T, int DH>
-hipError_t fwd_launch(const void* qkv, void* o, float* lse2, int mu, int S, int H, const DropArgs& drop,
-                      hipStream_t st) {
-  const int d = H * DH;
+hipError_t fwd_launch(const AttnArgs& a, void* o, float* lse2, hipStream_t st) {
+  const int mu = a.mu, S = a.S, H = a.H, d = H * DH;
   const float scale_log2 = LOG2E / sqrtf((float)DH);
-  if constexpr (sizeof(T) == 2) {
-    auto go = [&](auto small) {
-      constexpr bool SM = decltype(small)::value;
-      using C = FwdRing<DH, SM>;
-      dim3 grid(mu * H, (S + C::BQ - 1) / C::BQ);   // x fastest: every head's heaviest query block first
-      auto k = drop.thr ? attn_fwd_ring_kernel<DH, true, SM> : attn_fwd_ring_kernel<DH, false, SM>;
-      hipLaunchKernelGGL(k, grid, dim3(C::NTF), 0, st, reinterpret_cast<const bf16*>(qkv), reinterpret_cast<bf16*>(o),
-                         lse2, S, H, d, scale_log2, drop);
+  const size_t lds = bias_lds(a, 0);
+  T* out = reinterpret_cast<T*>(o);
+  auto launch = [&](auto bias) {
+    constexpr bool B = decltype(bias)::value;
+    if constexpr (sizeof(T) == 2) {
+      auto go = [&](auto small) {
+        constexpr bool SM = decltype(small)::value;
+        using C = FwdRing<DH, SM>;
+        dim3 grid(mu * H, (S + C::BQ - 1) / C::BQ);   // x fastest: every head's heaviest query block first
+        auto k = a.drop.thr ? attn_fwd_ring_kernel<DH, true, SM, B> : attn_fwd_ring_kernel<DH, false, SM, B>;
+        hipLaunchKernelGGL(k, grid, dim3(C::NTF), lds, st, view<T>(a), out, lse2, S, H, d, scale_log2, a.drop, bias_args(a));
+      };
+      if (small_grid(mu * H, S)) go(std::true_type{});
+      else go(std::false_type{});
+    } else {
+      auto k = a.drop.thr ? attn_fwd_kernel<T, DH, true, B> : attn_fwd_kernel<T, DH, false, B>;
+      hipLaunchKernelGGL(k, dim3((S + 63) / 64, mu * H), dim3(NT), lds, st, view<T>(a), out, lse2, S, H, d, scale_log2, a.drop,
+                         bias_args(a));
+    }
+    return hipGetLastError();
+  };
+  return a.table ? launch(std::true_type{}) : launch(std::false_type{});
+}
+
+// Query blocks of the dQ workgroups: 64 queries, or as many as the ring's larger ones take.
+template <int DH> int dq_rows(int64_t heads, int S) {
+  return small_grid(2 * heads, S) ? BwdRing<DH, true>::BR : BwdRing<DH, false>::BR;
+}
+int dq_blocks(const AttnArgs& a) {
+  const int64_t heads = (int64_t)a.mu * a.H;
+  int rows = 64;
+  if (a.dt == DT_BF16) rows = a.dh == 32 ? dq_rows<32>(heads, a.S) : a.dh == 64 ? dq_rows<64>(heads, a.S) : dq_rows<128>(heads, a.S);
+  return (a.S + rows - 1) / rows;
+}
+
+template <typename T, int DH>
+hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, const void* dO, const float* lse2, float* ws,
+                      hipStream_t st) {
+  const int mu = a.mu, S = a.S, H = a.H, d = H * DH;
+  const float scale = 1.f / sqrtf((float)DH);
+  const float scale_log2 = LOG2E * scale;
+  const T* g = reinterpret_cast<const T*>(dO);
+  const GradView<T> grad{reinterpret_cast<T*>(gr.dq), reinterpret_cast<T*>(gr.dk), reinterpret_cast<T*>(gr.dv), gr.ldq, gr.ldk,
+                         gr.ldv, gr.sum_q, gr.sum_k, gr.sum_v};
+  BiasArgs ba = bias_args(a);
+  if (a.table && gr.g_table) ba.part = ws + attn_bwd_workspace_floats(a.dt, mu, S, H);
+  const int64_t rows = (int64_t)mu * S * H;
+  auto launch = [&](auto bias) {
+    constexpr bool B = decltype(bias)::value;
+    if constexpr (sizeof(T) == 2) {
+      const int S_pad = (S + 63) / 64 * 64;
+      const int64_t threads = (rows + PAIR_ROWS - 1) / PAIR_ROWS * (DH / 8);
+      const int64_t pad_threads = (int64_t)mu * H * (S_pad - S);
+      const int64_t grid_threads = threads > pad_threads ? threads : pad_threads;
+      hipLaunchKernelGGL((attn_pairs_kernel<DH>), dim3((unsigned)((grid_threads + NT - 1) / NT)), dim3(NT), 0, st,
+                         reinterpret_cast<const bf16*>(o), g, lse2, ws, S, S_pad, H, d, rows, B);
+      hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      auto go = [&](auto small) {
+        constexpr bool SM = decltype(small)::value;
+        using C = BwdRing<DH, SM>;
+        const int ny = (S + C::BR - 1) / C::BR;
+        const dim3 grid(mu * H, 2 * ny);   // dK/dV blocks, then dQ blocks
+        auto k = a.drop.thr ? attn_bwd_ring_kernel<DH, true, SM, B> : attn_bwd_ring_kernel<DH, false, SM, B>;
+        hipLaunchKernelGGL(k, grid, dim3(C::NTB), bias_lds(a, C::WAVES), st, view<T>(a), g, ws, grad, S, S_pad, H, d,
+                           scale_log2, scale, a.drop, ny, ba);
+      };
+      if (small_grid(2 * (int64_t)mu * H, S)) go(std::true_type{});
+      else go(std::false_type{});
       return hipGetLastError();
-    };
-    return small_grid(mu * H, S) ? go(std::true_type{}) : go(std::false_type{});
-  }
-  dim3 grid((S + 63) / 64, mu * H);
-  if (drop.thr)
-    hipLaunchKernelGGL((attn_fwd_kernel<T, DH, true>), grid, dim3(NT), 0, st, reinterpret_cast<const T*>(qkv),
-                       reinterpret_cast<T*>(o), lse2, S, H, d, scale_log2, drop);
-  else
-    hipLaunchKernelGGL((attn_fwd_kernel<T, DH, false>), grid, dim3(NT), 0, st, reinterpret_cast<const T*>(qkv),
-                       reinterpret_cast<T*>(o), lse2, S, H, d, scale_log2, drop);
+    } else {
+      const int64_t threads = rows * (DH / Vec<T>::V);
+      hipLaunchKernelGGL((attn_dsum_kernel<T, DH>), dim3((unsigned)((threads + NT - 1) / NT)), dim3(NT), 0, st,
+                         reinterpret_cast<const T*>(o), g, ws, S, H, d, rows);
+      hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      auto dkdv = a.drop.thr ? attn_bwd_dkdv_kernel<T, DH, true, B> : attn_bwd_dkdv_kernel<T, DH, false, B>;
+      hipLaunchKernelGGL(dkdv, dim3((S + BKV - 1) / BKV, mu * H), dim3(NT), bias_lds(a, 0), st, view<T>(a), g, lse2, ws, grad,
+                         S, H, d, scale_log2, scale, a.drop, ba);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      auto dqk = a.drop.thr ? attn_bwd_dq_kernel<T, DH, true, B> : attn_bwd_dq_kernel<T, DH, false, B>;
+      hipLaunchKernelGGL(dqk, dim3((S + 63) / 64, mu * H), dim3(NT), bias_lds(a, NT / 64), st, view<T>(a), g, lse2, ws, grad, S,
+                         H, d, scale_log2, scale, a.drop, ba);
+      e = hipGetLastError();
+      // column sums: one pass where all three lie side by side
+      if (e == hipSuccess && gr.sum_q != nullptr && gr.sum_k == gr.sum_q + d && gr.sum_v == gr.sum_k + d &&
+          gr.ldk == gr.ldq && gr.ldv == gr.ldq && grad.k == grad.q + d && grad.v == grad.k + d)
+        return colsum_acc(DT_F32, gr.dq, gr.ldq, mu * S, 3 * d, gr.sum_q, st);   // of this lambda
+      if (e == hipSuccess && gr.sum_q != nullptr) e = colsum_acc(DT_F32, gr.dq, gr.ldq, mu * S, d, gr.sum_q, st);
+      if (e == hipSuccess && gr.sum_k != nullptr) e = colsum_acc(DT_F32, gr.dk, gr.ldk, mu * S, d, gr.sum_k, st);
+      if (e == hipSuccess && gr.sum_v != nullptr) e = colsum_acc(DT_F32, gr.dv, gr.ldv, mu * S, d, gr.sum_v, st);
+      return e;
+    }
+  };
+  hipError_t e = a.table ? launch(std::true_type{}) : launch(std::false_type{});
+  if (e != hipSuccess || ba.part == nullptr) return e;
+  hipLaunchKernelGGL(attn_bias_sums_kernel, dim3(H), dim3(BS_NT), 0, st, ba.part, mu, dq_blocks(a), H, a.bounds, a.n_buckets,
+                     a.max_distance, gr.g_table);
   return hipGetLastError();
 }
 
-template <typename T, int DH>
-hipError_t bwd_launch(const void* qkv, const void* o, const void* dO, const float* lse2, float* Dbuf, void* dqkv,
-                      float* gbias, int mu, int S, int H, const DropArgs& drop, hipStream_t st) {
-  const int d = H * DH;
-  const float scale = 1.f / sqrtf((float)DH);
-  const float scale_log2 = LOG2E * scale;
-  if constexpr (sizeof(T) == 2) {
-    const int S_pad = (S + 63) / 64 * 64;
-    const int64_t rows = (int64_t)mu * S * H;
-    const int64_t threads = (rows + PAIR_ROWS - 1) / PAIR_ROWS * (DH / 8);
-    const bf16* q = reinterpret_cast<const bf16*>(qkv);
-    const bf16* g = reinterpret_cast<const bf16*>(dO);
-    bf16* dq = reinterpret_cast<bf16*>(dqkv);
-    const int64_t pad_threads = (int64_t)mu * H * (S_pad - S);
-    const int64_t grid_threads = threads > pad_threads ? threads : pad_threads;
-    hipLaunchKernelGGL((attn_pairs_kernel<DH>), dim3((unsigned)((grid_threads + NT - 1) / NT)), dim3(NT), 0, st,
-                       reinterpret_cast<const bf16*>(o), g, lse2, Dbuf, S, S_pad, H, d, rows);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    auto go = [&](auto small) {
-      constexpr bool SM = decltype(small)::value;
-      using C = BwdRing<DH, SM>;
-      const int ny = (S + C::BR - 1) / C::BR;
-      const dim3 grid(mu * H, 2 * ny);   // dK/dV blocks, then dQ blocks
-      auto k = drop.thr ? attn_bwd_ring_kernel<DH, true, SM> : attn_bwd_ring_kernel<DH, false, SM>;
-      hipLaunchKernelGGL(k, grid, dim3(C::NTB), 0, st, q, g, Dbuf, dq, S, S_pad, H, d, scale_log2, scale, gbias, drop, ny);
-      return hipGetLastError();
-    };
-    return small_grid(2 * mu * H, S) ? go(std::true_type{}) : go(std::false_type{});
-  }
-  constexpr int LPR = DH / Vec<T>::V;
-  const int64_t rows = (int64_t)mu * S * H;
-  const int64_t threads = rows * LPR;
-  hipLaunchKernelGGL((attn_dsum_kernel<T, DH>), dim3((unsigned)((threads + NT - 1) / NT)), dim3(NT), 0, st,
-                     reinterpret_cast<const T*>(o), reinterpret_cast<const T*>(dO), Dbuf, S, H, d, rows);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  auto dkdv = drop.thr ? attn_bwd_dkdv_kernel<T, DH, true> : attn_bwd_dkdv_kernel<T, DH, false>;
-  hipLaunchKernelGGL(dkdv, dim3((S + BKV - 1) / BKV, mu * H), dim3(NT), 0, st,
-                     reinterpret_cast<const T*>(qkv), reinterpret_cast<const T*>(dO), lse2, Dbuf,
-                     reinterpret_cast<T*>(dqkv), S, H, d, scale_log2, scale, drop);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  auto dqk = drop.thr ? attn_bwd_dq_kernel<T, DH, true> : attn_bwd_dq_kernel<T, DH, false>;
-  hipLaunchKernelGGL(dqk, dim3((S + 63) / 64, mu * H), dim3(NT), 0, st,
-                     reinterpret_cast<const T*>(qkv), reinterpret_cast<const T*>(dO), lse2, Dbuf,
-                     reinterpret_cast<T*>(dqkv), S, H, d, scale_log2, scale, drop);
-  e = hipGetLastError();
-  if (e != hipSuccess || gbias == nullptr) return e;
-  return colsum_acc(sizeof(T) == 2 ? DT_BF16 : DT_F32, dqkv, 3 * d, mu * S, 3 * d, gbias, st);
-}
-
-template <typename T>
-hipError_t fwd_dh(const void* qkv, void* o, float* lse2, int mu, int S, int H, int dh, const DropArgs& drop,
-                  hipStream_t st) {
-  switch (dh) {
-    case 32: return fwd_launch<T, 32>(qkv, o, lse2, mu, S, H, drop, st);
-    case 64: return fwd_launch<T, 64>(qkv, o, lse2, mu, S, H, drop, st);
-    case 128:
-      // fp32 at head_dim 128 would exceed the 64 KiB LDS budget of these tilings
-      if constexpr (sizeof(T) == 2) return fwd_launch<T, 128>(qkv, o, lse2, mu, S, H, drop, st);
-      break;
-  }
-  return hipErrorInvalidValue;
-}
-
-template <typename T>
-hipError_t bwd_dh(const void* qkv, const void* o, const void* dO, const float* lse2, float* Dbuf, void* dqkv,
-                  float* gbias, int mu, int S, int H, int dh, const DropArgs& drop, hipStream_t st) {
-  switch (dh) {
-    case 32: return bwd_launch<T, 32>(qkv, o, dO, lse2, Dbuf, dqkv, gbias, mu, S, H, drop, st);
-    case 64: return bwd_launch<T, 64>(qkv, o, dO, lse2, Dbuf, dqkv, gbias, mu, S, H, drop, st);
-    case 128:
-      if constexpr (sizeof(T) == 2)
-        return bwd_launch<T, 128>(qkv, o, dO, lse2, Dbuf, dqkv, gbias, mu, S, H, drop, st);
-      break;
-  }
-  return hipErrorInvalidValue;
+bool attn_args_ok(const AttnArgs& a) {
+  if (a.mu <= 0 || a.S <= 0 || a.H <= 0) return false;
+  return !a.table || (a.bounds && a.n_buckets >= 1 && a.n_buckets <= MAX_BUCKETS && a.max_distance >= 1 &&
+                      a.max_distance <= MAX_DISTANCE);
 }
 
 }  // namespace
 
-hipError_t attn_fwd(DType dt, const void* qkv, void* o, float* lse2, int mu, int S, int H, int dh, const DropArgs& drop,
-                    hipStream_t st) {
-  if (mu <= 0 || S <= 0 || H <= 0) return hipErrorInvalidValue;
-  if (dt == DT_BF16) return fwd_dh<bf16>(qkv, o, lse2, mu, S, H, dh, drop, st);
-  return fwd_dh<float>(qkv, o, lse2, mu, S, H, dh, drop, st);
+// fp32 at head_dim 128 would exceed the 64 KiB LDS budget of its tilings
+hipError_t attn_fwd(const AttnArgs& a, void* o, float* lse2, hipStream_t st) {
+  if (!attn_args_ok(a)) return hipErrorInvalidValue;
+  if (a.dt == DT_BF16) {
+    if (a.dh == 32) return fwd_launch<bf16, 32>(a, o, lse2, st);
+    if (a.dh == 64) return fwd_launch<bf16, 64>(a, o, lse2, st);
+    if (a.dh == 128) return fwd_launch<bf16, 128>(a, o, lse2, st);
+    return hipErrorInvalidValue;
+  }
+  if (a.dh == 32) return fwd_launch<float, 32>(a, o, lse2, st);
+  if (a.dh == 64) return fwd_launch<float, 64>(a, o, lse2, st);
+  return hipErrorInvalidValue;
 }
 
 int64_t attn_bwd_workspace_floats(DType dt, int mu, int S, int H) {
   if (dt == DT_BF16) return 2 * (int64_t)mu * H * ((S + 63) / 64 * 64);
   return (int64_t)mu * H * S;
 }
+int64_t attn_bias_workspace_floats(const AttnArgs& a) {
+  return (int64_t)a.mu * a.H * dq_blocks(a) * (a.max_distance + 1);
+}
 
-hipError_t attn_bwd(DType dt, const void* qkv, const void* o, const void* dO, const float* lse2, float* Dbuf,
-                    void* dqkv, float* gbias, int mu, int S, int H, int dh, const DropArgs& drop, hipStream_t st) {
-  if (mu <= 0 || S <= 0 || H <= 0) return hipErrorInvalidValue;
-  if (dt == DT_BF16) return bwd_dh<bf16>(qkv, o, dO, lse2, Dbuf, dqkv, gbias, mu, S, H, dh, drop, st);
-  return bwd_dh<float>(qkv, o, dO, lse2, Dbuf, dqkv, gbias, mu, S, H, dh, drop, st);
+hipError_t attn_bwd(const AttnArgs& a, const AttnGrads& g, const void* o, const void* dO, const float* lse2, float* ws,
+                    hipStream_t st) {
+  if (!attn_args_ok(a)) return hipErrorInvalidValue;
+  if (a.dt == DT_BF16) {
+    if (a.dh == 32) return bwd_launch<bf16, 32>(a, g, o, dO, lse2, ws, st);
+    if (a.dh == 64) return bwd_launch<bf16, 64>(a, g, o, dO, lse2, ws, st);
+    if (a.dh == 128) return bwd_launch<bf16, 128>(a, g, o, dO, lse2, ws, st);
+    return hipErrorInvalidValue;
+  }
+  if (a.dh == 32) return bwd_launch<float, 32>(a, g, o, dO, lse2, ws, st);
+  if (a.dh == 64) return bwd_launch<float, 64>(a, g, o, dO, lse2, ws, st);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace paci

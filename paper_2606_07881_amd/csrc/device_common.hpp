@@ -207,14 +207,14 @@ __device__ __forceinline__ void st16g(void* p, const u32x4& v) { *(__attribute__
 // K-major source: element (row r, contracted c) at src[r * ld + c]. Stages rows
 // [0, ROWS) and contracted vectors [0, KVN); rows >= rows_valid read as zero.
 template <typename T, int ROWS, int KVN, int NT>
-__device__ __forceinline__ void stage_kmajor(u32x4* tile, const T* src, int ld, int rows_valid) {
+__device__ __forceinline__ void stage_kmajor(u32x4* tile, const T* src, int64_t ld, int rows_valid) {
   constexpr int V = Vec<T>::V;
   constexpr int ITEMS = ROWS * KVN;
 #pragma unroll
   for (int it = threadIdx.x; it < ITEMS; it += NT) {
     const int kv = it % KVN, r = it / KVN;
     u32x4 v = {0, 0, 0, 0};
-    if (r < rows_valid) v = ld16(src + (size_t)r * ld + kv * V);
+    if (r < rows_valid) v = ld16(src + r * ld + kv * V);
     tile[lds_slot<ROWS>(kv, r)] = v;
   }
 }
@@ -224,7 +224,7 @@ __device__ __forceinline__ void stage_kmajor(u32x4* tile, const T* src, int ld, 
 // 0 .. KVN*V-1 that keeps each MFMA step's 4*V indices together). Contracted
 // indices >= c_valid read as zero. Rows [0, ROWS) must be in bounds.
 template <typename T, int ROWS, int KVN, int NT, class Perm>
-__device__ __forceinline__ void stage_mnmajor(u32x4* tile, const T* src, int ld, int c_valid, Perm perm) {
+__device__ __forceinline__ void stage_mnmajor(u32x4* tile, const T* src, int64_t ld, int c_valid, Perm perm) {
   constexpr int V = Vec<T>::V;
   constexpr int ITEMS = (ROWS / V) * KVN;
   for (int it = threadIdx.x; it < ITEMS; it += NT) {
@@ -233,7 +233,7 @@ __device__ __forceinline__ void stage_mnmajor(u32x4* tile, const T* src, int ld,
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int c = perm(kv, j);
-      in[j] = (c < c_valid) ? ld16(src + (size_t)c * ld + rb * V) : u32x4{0, 0, 0, 0};
+      in[j] = (c < c_valid) ? ld16(src + c * ld + rb * V) : u32x4{0, 0, 0, 0};
     }
     transpose_block<T>(in, out);
 #pragma unroll
@@ -283,6 +283,16 @@ __device__ __forceinline__ float dpp_f(float v) {
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_u(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+// A move within the 16 lanes that may run past them: 0 comes in (CTRL 0x100 + n:
+// lane c takes lane c + n; 0x110 + n: lane c takes lane c - n).
+template <int CTRL>
+__device__ __forceinline__ float dpp_shift(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+// Adds v to a float in LDS (one instruction, no result).
+__device__ __forceinline__ void lds_add(float* p, float v) {
+  (void)__hip_atomic_fetch_add((__attribute__((address_space(3))) float*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 __device__ __forceinline__ float row_sum16(float v) {
   v += dpp_f<0xB1>(v);    // quad_perm [1, 0, 3, 2]

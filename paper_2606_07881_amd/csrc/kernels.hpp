@@ -10,6 +10,8 @@ enum DType { DT_F32 = 0, DT_BF16 = 1 };
 
 // Compute units of the current device (256 if it cannot be asked).
 int cu_count();
+// The status that paci_last_hip_error(NULL) reports (calls without a handle).
+void note_hip_error(hipError_t e);
 
 // Dropout at one site of one micro-batch: key (seed, mb), site word
 // (block << 2) | site (0 embedding, 1 attention probabilities, 2 projection
@@ -131,16 +133,73 @@ KmajorPlan gemm_kmajor_plan(int M, int N);
 struct WindowPlan { int bn, splits; };
 WindowPlan gemm_window_plan(int M, int N, int64_t K);
 
-// ---- causal attention over the fused projection qkv [T, 3d] --------------------------
-// Forward: o [T, d]; lse2 [mu*H*S] = log2-sum-exp2 of the scaled scores in log2 units.
-hipError_t attn_fwd(DType dt, const void* qkv, void* o, float* lse2, int mu, int S, int H, int dh, const DropArgs& drop,
-                    hipStream_t st);
-// Backward: D = rowsum(dO * O) per (b, h, query), then dK, dV and dQ into dqkv [T, 3d].
-// Dbuf is workspace of attn_bwd_workspace_floats() floats. gbias (optional, fp32 [3d]):
-// += the column sums of dqkv, i.e. the gradient of the qkv projection's bias.
+// ---- norms and rotation of the query and key heads ---------------------------------------
+// T rows of q_heads + k_heads heads of dh elements (row strides in elements). Forward:
+// out = rot(x / sqrt(mean(x^2) + eps) * gain), the first rope_dims elements of every head
+// turned by pos * freq; norm false: no norm; rope_dims 0: no rotation. pos null: row t
+// is position t % seq. Backward: out = dL/dx from dy = dL/d(forward's out) and its x
+// (not read without norm), g_gain_q / g_gain_k (nullable) += gain gradients, g_bias
+// (nullable) += column sums of out; ws: rotary_workspace_floats(). out may be x
+// (forward) or dy (backward).
+// dh and rope_dims multiples of 16, dh <= 256; 16-byte aligned rows.
+struct RotArgs {
+  DType dt = DT_F32;
+  int T = 0, seq = 1, q_heads = 0, k_heads = 0, dh = 0, rope_dims = 0;
+  bool norm = false;
+  bool adjacent = false;   // pairs (2i, 2i + 1) instead of (i, i + rope_dims / 2)
+  float eps = 0.f;
+  const void* x = nullptr; int64_t ldx = 0;
+  const void* dy = nullptr; int64_t lddy = 0;
+  void* out = nullptr; int64_t ldout = 0;
+  const float* gain_q = nullptr;
+  const float* gain_k = nullptr;
+  const int32_t* pos = nullptr;
+  const double* freq = nullptr;
+  float* g_gain_q = nullptr;
+  float* g_gain_k = nullptr;
+  float* g_bias = nullptr;
+  float* ws = nullptr;
+};
+int64_t rotary_workspace_floats(const RotArgs& r);
+hipError_t rotary(const RotArgs& r, bool bwd, hipStream_t st);
+
+// ---- causal attention ---------------------------------------------------------------------
+// mu sequences of S tokens, H heads of dh; row t of q at q + t ldq (elements), head h at
+// + h dh, likewise k and v. With a table, score (i, j) adds table[bucket(i - j)][h], where
+// bucket(n) counts the bounds[1 .. n_buckets - 1] at or below min(n, max_distance);
+// entries at or below -1e30 hide their distances.
+constexpr int MAX_BUCKETS = 256, MAX_DISTANCE = 512;
+struct AttnArgs {
+  DType dt = DT_F32;
+  int mu = 0, S = 0, H = 0, dh = 0;
+  const void* q = nullptr; int64_t ldq = 0;
+  const void* k = nullptr; int64_t ldk = 0;
+  const void* v = nullptr; int64_t ldv = 0;
+  DropArgs drop;
+  const float* table = nullptr;       // [n_buckets][H]
+  const int32_t* bounds = nullptr;    // device, ascending
+  int n_buckets = 0, max_distance = 0;
+};
+// Gradients, rows as the operands'. sum_q, sum_k, sum_v (nullable; bf16: sum_k only with
+// sum_v): += their column sums (H dh floats each). g_table (nullable): += the table's gradient.
+struct AttnGrads {
+  void* dq = nullptr; int64_t ldq = 0;
+  void* dk = nullptr; int64_t ldk = 0;
+  void* dv = nullptr; int64_t ldv = 0;
+  float* sum_q = nullptr;
+  float* sum_k = nullptr;
+  float* sum_v = nullptr;
+  float* g_table = nullptr;
+};
+// Forward: o [T, H dh]; lse2 [mu*H*S] = log2-sum-exp2 of the scaled (and biased) scores in
+// log2 units. A query with no key left has o = 0 and lse2 = -inf.
+hipError_t attn_fwd(const AttnArgs& a, void* o, float* lse2, hipStream_t st);
+// Backward: D = rowsum(dO * O) per (b, h, query), then dK, dV and dQ. ws is workspace of
+// attn_bwd_workspace_floats() floats, followed by attn_bias_workspace_floats() for g_table.
 int64_t attn_bwd_workspace_floats(DType dt, int mu, int S, int H);
-hipError_t attn_bwd(DType dt, const void* qkv, const void* o, const void* dO, const float* lse2, float* Dbuf,
-                    void* dqkv, float* gbias, int mu, int S, int H, int dh, const DropArgs& drop, hipStream_t st);
+int64_t attn_bias_workspace_floats(const AttnArgs& a);   // reads dt, mu, S, H, dh, max_distance
+hipError_t attn_bwd(const AttnArgs& a, const AttnGrads& g, const void* o, const void* dO, const float* lse2, float* ws,
+                    hipStream_t st);
 
 // ---- LayerNorm -----------------------------------------------------------------------
 // n = (x - mean) * rstd * gamma + beta, per row of d; xcopy (optional) receives x.

@@ -37,6 +37,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <mutex>
 #include <new>
@@ -53,8 +54,9 @@ struct paci_fsm {
   int K, delay, t, c, q, next_f, next_b;
 };
 
-// HIP status of the last failed call that had no handle to record it in (init).
-static int g_init_hip_error = 0;
+// HIP status of the last failed call that had no handle to record it in (init, the operator calls).
+static std::atomic<int> g_init_hip_error{0};
+void paci::note_hip_error(hipError_t e) { g_init_hip_error = (int)e; }
 
 // ---- static scratch of the allocation-free backward ----------------------------------------
 // paci_stage_backward_static takes the attention backward's per-query (lse2, D)
@@ -759,6 +761,24 @@ double attn_pairs(const paci_shapes& s) {
   return (double)s.micro_batch * s.n_heads * ((double)s.seq * (s.seq + 1) / 2.0);
 }
 
+// The attention of block l: q, k and v as the activation area sl holds them.
+paci::AttnArgs attn_args(const paci_stage* h, const char* sl, int l, int mb) {
+  const paci_shapes& s = h->s;
+  const size_t d = s.d_model;
+  paci::AttnArgs a;
+  a.dt = h->dt;
+  a.mu = s.micro_batch;
+  a.S = s.seq;
+  a.H = s.n_heads;
+  a.dh = s.head_dim;
+  a.q = sl + h->L.blk[l].qkv;
+  a.k = sl + h->L.blk[l].qkv + d * h->esz;
+  a.v = sl + h->L.blk[l].qkv + 2 * d * h->esz;
+  a.ldq = a.ldk = a.ldv = 3 * (int64_t)d;
+  a.drop = h->drop(mb, l, SITE_ATTN);
+  return a;
+}
+
 // ---- forward of the block stack -----------------------------------------------------------------
 // in: block-0 input (stage input or embedding output); x0_copy: where to store a
 // copy of it (nullptr: `in` stays valid), which block 0's residual then reads.
@@ -774,8 +794,7 @@ int blocks_fwd(paci_stage* h, char* sl, const void* in, void* x0_copy, void* out
     TRY(ln_fwd(h, x, sl + o.n1, mean1, rstd1, b.ln1_g, b.ln1_b, l == 0 ? x0_copy : nullptr));
     TRY(linear_fwd(h, sl + o.n1, b.w_qkv, b.b_qkv, T, 3 * d, d, paci::EPI_BIAS, sl + o.qkv, nullptr, nullptr));
     TRY(run(h, F_ATTN_FWD, 4.0 * attn_pairs(s) * s.head_dim, [&] {
-      return paci::attn_fwd(h->dt, sl + o.qkv, sl + o.o, reinterpret_cast<float*>(sl + o.lse2), s.micro_batch, s.seq,
-                            s.n_heads, s.head_dim, h->drop(mb, l, SITE_ATTN), h->st);
+      return paci::attn_fwd(attn_args(h, sl, l, mb), sl + o.o, reinterpret_cast<float*>(sl + o.lse2), h->st);
     }));
     const void* res = l > 0 ? (const void*)(sl + o.x) : (x0_copy ? (const void*)x0_copy : in);
     char* zd = h->L.dropout ? h->ws(h->L.w_zdrop) : nullptr;   // a branch output before its dropout
@@ -853,9 +872,16 @@ int block_bwd(paci_stage* h, char* sl, int l, const void* dy, void* dx, bool dy_
   TRY(linear_dgrad(h, dx1, d, b.w_o, T, d, d, paci::EPI_STORE, dO, nullptr));
   // attention; G_bqkv += sum dqkv in the same kernels
   TRY(run(h, F_ATTN_BWD, 8.0 * attn_pairs(s) * s.head_dim, [&] {
-    return paci::attn_bwd(h->dt, sl + o.qkv, sl + o.o, dO, reinterpret_cast<const float*>(sl + o.lse2),
-                          h->pairs, dqkv, h->g(b.b_qkv), s.micro_batch, s.seq,
-                          s.n_heads, s.head_dim, h->drop(mb, l, SITE_ATTN), h->st);
+    paci::AttnGrads gr;
+    gr.dq = dqkv;
+    gr.dk = dqkv + (size_t)d * h->esz;
+    gr.dv = dqkv + 2 * (size_t)d * h->esz;
+    gr.ldq = gr.ldk = gr.ldv = 3 * d;
+    gr.sum_q = h->g(b.b_qkv);
+    gr.sum_k = gr.sum_q + d;
+    gr.sum_v = gr.sum_k + d;
+    return paci::attn_bwd(attn_args(h, sl, l, mb), gr, sl + o.o, dO, reinterpret_cast<const float*>(sl + o.lse2), h->pairs,
+                          h->st);
   }));
   // qkv = n1 Wqkv^T + bqkv
   if (!win) TRY(linear_wgrad(h, dqkv, 3 * d, sl + o.n1, d, 3 * d, d, T, b.w_qkv));
@@ -1519,7 +1545,7 @@ extern "C" int paci_stage_sync(paci_stage* h) {
   return PACI_OK;
 }
 
-extern "C" int paci_last_hip_error(const paci_stage* h) { return h ? h->last_hip : g_init_hip_error; }
+extern "C" int paci_last_hip_error(const paci_stage* h) { return h ? h->last_hip : g_init_hip_error.load(); }
 
 extern "C" const char* paci_strerror(int status) {
   switch (status) {
