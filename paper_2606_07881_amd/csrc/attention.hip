@@ -96,6 +96,23 @@ template <int NTH> __device__ __forceinline__ void bias_build(float* vec, const 
   __syncthreads();
 }
 
+// How a block's scores get their bias: none; one value for the whole block (its distances
+// all reach max_distance); or each from the vector.
+using NoBias = std::integral_constant<int, 0>;
+using FarBias = std::integral_constant<int, 1>;
+using VecBias = std::integral_constant<int, 2>;
+// The one value, and the least distance of a block from which it serves: max_distance, or
+// never where adding it to the score first is not the same as adding it to the exponent
+// (a hidden, NaN or huge entry).
+struct FarValue {
+  float b;
+  int from;
+};
+__device__ __forceinline__ FarValue bias_far(const float* vec, int max_distance) {
+  const float b = as_float(__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, vec[BIAS_FRONT + max_distance])));
+  return {b, fabsf(b) <= 1024.f ? max_distance : 0x7fffffff};
+}
+
 // Sums over the diagonals of dS. acc[i][r] of lane (g = l / 16, c = l % 16) holds the
 // sum over a block's tiles with qs - kt = i - 3 (query tile minus key tile) at distance
 // 16 (i - 3) + c - 4 g - r from the block's own. Moving the r-th value by r lanes within
@@ -413,13 +430,15 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   };
   // online softmax of block kb's scores: running max and sum, rescaled
   // accumulators, and the probabilities (dropped ones zeroed) as bf16 fragments
-  auto softmax = [&](auto masked, int kb, floatx4 (&sc)[QS][4], u32x4 (&pf)[QS][2]) {
+  FarValue far{0.f, 0};
+  auto softmax = [&](auto masked, auto mode, int kb, floatx4 (&sc)[QS][4], u32x4 (&pf)[QS][2]) {
+    constexpr bool VEC = decltype(mode)::value == 2, FAR = decltype(mode)::value == 1;
     const int k0 = kb * BKV;
-    const float* bp = BIAS ? bvec + BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) + (l & 15) - 4 * g : nullptr;
+    const float* bp = VEC ? bvec + BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) + (l & 15) - 4 * g : nullptr;
 #pragma unroll
     for (int qs = 0; qs < QS; ++qs) {
       const int qrow = qw0 + 16 * qs + (l & 15);
-      if constexpr (BIAS) {
+      if constexpr (VEC) {
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
@@ -440,14 +459,15 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
 #pragma unroll
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[qs][kt][r]);
       mx = group4_max(mx);
-      const float m_new = fmaxf(m_run[qs], BIAS ? mx : mx * scale_log2);
+      const float m_new = fmaxf(m_run[qs], VEC ? mx : FAR ? fmaf(mx, scale_log2, far.b) : mx * scale_log2);
       const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
       const float alpha = fast_exp2(m_run[qs] - m_use);
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          sc[qs][kt][r] = fast_exp2(BIAS ? sc[qs][kt][r] - m_use : fmaf(sc[qs][kt][r], scale_log2, -m_use));
+          sc[qs][kt][r] = fast_exp2(VEC ? sc[qs][kt][r] - m_use
+                                        : fmaf(sc[qs][kt][r], scale_log2, FAR ? far.b - m_use : -m_use));
       if constexpr (BIAS) {
         float rs = 0.f;
 #pragma unroll
@@ -515,13 +535,12 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
     if (kb + NS - 1 < nkb) fill(kb + NS - 1);
     if (kb > my_last) return;
     u32x4 pf[QS][2];
-    if constexpr (!PIPE) {
-      scores(kb, cur);
-      if (kb < my_last) softmax(std::false_type{}, kb, cur, pf);
-      else softmax(std::true_type{}, kb, cur, pf);
-    } else if (kb < my_last) {
+    // with a bias, a block whose distances reach far.from takes the one value
+    using Near = std::conditional_t<BIAS, VecBias, NoBias>;
+    const bool near = !BIAS || qw0 - kb * BKV - (BKV - 1) < far.from;
+    auto inner = [&](auto mode) {
       scores(kb + 1, nxt);
-      softmax(std::false_type{}, kb, cur, pf);
+      softmax(std::false_type{}, mode, kb, cur, pf);
       // interleave: the fragment reads first, then one MFMA per few ALU instructions
       __builtin_amdgcn_sched_group_barrier(0x100, 4 * KS, 0);
 #pragma unroll
@@ -529,8 +548,18 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
       }
-    } else {
-      softmax(std::true_type{}, kb, cur, pf);
+    };
+    if constexpr (!PIPE) {
+      scores(kb, cur);
+      if (kb >= my_last) softmax(std::true_type{}, Near{}, kb, cur, pf);
+      else if (near) softmax(std::false_type{}, Near{}, kb, cur, pf);
+      else softmax(std::false_type{}, FarBias{}, kb, cur, pf);
+    } else if (kb >= my_last) {
+      softmax(std::true_type{}, Near{}, kb, cur, pf);
+    } else if (near) {
+      inner(Near{});
+    } else if constexpr (BIAS) {
+      inner(FarBias{});
     }
     pv(kb, pf);
   };
@@ -543,7 +572,10 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   // compiler sees: it then knows qf has landed and puts no vmcnt(0) in the
   // loop, which would also wait for the ring's prefetches
   wait_vmcnt_all();
-  if constexpr (BIAS) bias_build<C::NTF>(bvec, bias, h, H);
+  if constexpr (BIAS) {
+    bias_build<C::NTF>(bvec, bias, h, H);
+    far = bias_far(bvec, bias.max_distance);
+  }
   barrier_no_fence();
   if (PIPE && my_last >= 0) scores(0, sA);
   for (int kb = 0; kb < nkb; kb += 2) {
@@ -956,7 +988,11 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
   for (int t = 0; t < NS - 1; ++t)
     if (t < njobs) fill(t);
   wait_vmcnt_all();   // kf and vf known complete: no vmcnt(0) inside the loop
-  if constexpr (BIAS) bias_build<C::NTB>(bvec, bias, h, H);
+  FarValue far{0.f, 0};
+  if constexpr (BIAS) {
+    bias_build<C::NTB>(bvec, bias, h, H);
+    far = bias_far(bvec, bias.max_distance);
+  }
   for (int j = 0; j < njobs; ++j) {
     wait_loads<C::L, NS - 2>(min(njobs - 1, j + NS - 2) - j);
     wait_lds_reads();
@@ -996,17 +1032,18 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
       // Dropout M = keep * scale: dV takes P M, and dP = (dO V^T) M.
       uint32_t dbits[2][SUB];
       if constexpr (DROP) drop_col4_quad<SUB>(drop, bh, q0 + 32 * s, kw0, dbits);
-      auto softmax = [&](auto masked) {
+      auto softmax = [&](auto masked, auto mode) {
+        constexpr bool VEC = decltype(mode)::value == 2, FAR = decltype(mode)::value == 1;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int qi = (2 * s + u) * 16 + 4 * g + r;
-            const float lq = sP[2 * qi], Dq = sP[2 * qi + 1];
+            const float lq = FAR ? sP[2 * qi] - far.b : sP[2 * qi], Dq = sP[2 * qi + 1];
 #pragma unroll
             for (int ks = 0; ks < SUB; ++ks) {
-              float x = BIAS ? fmaf(sc[ks][u][r], scale_log2, bp[16 * (2 * s + u - ks) + r]) - lq
-                             : fmaf(sc[ks][u][r], scale_log2, -lq);
+              float x = VEC ? fmaf(sc[ks][u][r], scale_log2, bp[16 * (2 * s + u - ks) + r]) - lq
+                            : fmaf(sc[ks][u][r], scale_log2, -lq);
               if constexpr (decltype(masked)::value) {
                 const int key = kw0 + 16 * ks + (l & 15);
                 x = (key <= q0 + qi && q0 + qi < S && key < S) ? x : -INFINITY;
@@ -1023,8 +1060,10 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
             }
           }
       };
-      if (edge) softmax(std::true_type());
-      else softmax(std::false_type());
+      using Near = std::conditional_t<BIAS, VecBias, NoBias>;
+      if (edge) softmax(std::true_type(), Near{});
+      else if (!BIAS || q0 - kw0 - (C::WR - 1) < far.from) softmax(std::false_type(), Near{});
+      else if constexpr (BIAS) softmax(std::false_type(), FarBias{});
       u32x4 pfr[SUB], dsf[SUB];
 #pragma unroll
       for (int ks = 0; ks < SUB; ++ks) {
@@ -1135,11 +1174,14 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
     if (t < nkb) fill(t);
   wait_vmcnt_all();   // qf, gf, lq and Dq known complete: no vmcnt(0) inside the loop
   float* sums = nullptr;   // this wavefront's sums of dS by distance
+  float far_sum[4] = {0.f, 0.f, 0.f, 0.f};   // and over blocks beyond max_distance
+  FarValue far{0.f, 0};
   if constexpr (BIAS) {
     sums = bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets;
     for (int i = threadIdx.x; i < C::WAVES * bias_len(bias.max_distance); i += C::NTB) sums[i] = 0.f;
     sums += w * bias_len(bias.max_distance);
     bias_build<C::NTB>(bvec, bias, h, H);
+    far = bias_far(bvec, bias.max_distance);
   }
   for (int kb = 0; kb < nkb; ++kb) {
     wait_loads<C::L, NS - 2>(min(nkb - 1, kb + NS - 2) - kb);
@@ -1151,6 +1193,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
     const u32x4* sV = sK + C::BLK;
     const int k0 = kb * BKV;
     const bool edge = (k0 + BKV - 1 > qw0) || (k0 + BKV > S) || (qw0 + C::WR > S);
+    const bool near = !BIAS || edge || qw0 - k0 - (BKV - 1) < far.from;
     const int dist = BIAS ? BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) : 0;   // entry of the block's own distance
     const float* bp = BIAS ? bvec + dist + (l & 15) - 4 * g : nullptr;
     float diag[SUB + 3][4];
@@ -1181,9 +1224,11 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
           }
         }
       }
-      auto softmax = [&](auto masked) {
+      auto softmax = [&](auto masked, auto mode) {
+        constexpr bool VEC = decltype(mode)::value == 2, FAR = decltype(mode)::value == 1;
 #pragma unroll
         for (int qs = 0; qs < SUB; ++qs) {
+          const float lqb = FAR ? lq[qs] - far.b : lq[qs];
           const int q = qw0 + 16 * qs + (l & 15);
           uint32_t dbits[2] = {0xfu, 0xfu};   // dropout M = keep * scale on dP = dO V^T
           if constexpr (DROP) drop_row4_pair(drop, bh, q, k0 + 32 * s + 4 * g, k0 + 32 * s + 16 + 4 * g, dbits[0], dbits[1]);
@@ -1192,8 +1237,8 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
             const uint32_t bits = dbits[u];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float x = BIAS ? fmaf(sc[qs][u][r], scale_log2, bp[16 * (qs - 2 * s - u) - r]) - lq[qs]
-                             : fmaf(sc[qs][u][r], scale_log2, -lq[qs]);
+              float x = VEC ? fmaf(sc[qs][u][r], scale_log2, bp[16 * (qs - 2 * s - u) - r]) - lqb
+                            : fmaf(sc[qs][u][r], scale_log2, -lqb);
               if constexpr (decltype(masked)::value) {
                 const int key = k0 + (2 * s + u) * 16 + 4 * g + r;
                 x = (key <= q && key < S && q < S) ? x : -INFINITY;
@@ -1201,13 +1246,16 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
               const float p = fast_exp2(x);
               const float mk = DROP ? (((bits >> r) & 1) ? drop.scale : 0.f) : 1.f;
               dp[qs][u][r] = p * (dp[qs][u][r] * mk - Dq[qs]);
-              if constexpr (BIAS) diag[qs - 2 * s - u + 3][r] += dp[qs][u][r];
+              if constexpr (VEC) diag[qs - 2 * s - u + 3][r] += dp[qs][u][r];
+              if constexpr (FAR) far_sum[r] += dp[qs][u][r];
             }
           }
         }
       };
-      if (edge) softmax(std::true_type());
-      else softmax(std::false_type());
+      using Near = std::conditional_t<BIAS, VecBias, NoBias>;
+      if (edge) softmax(std::true_type(), Near{});
+      else if (near) softmax(std::false_type(), Near{});
+      else if constexpr (BIAS) softmax(std::false_type(), FarBias{});
       u32x4 dsf[SUB];
 #pragma unroll
       for (int qs = 0; qs < SUB; ++qs) dsf[qs] = acc_to_frag<bf16>(dp[qs], 0);
@@ -1219,7 +1267,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
       }
     }
     if constexpr (BIAS) {
-      if (bias.part != nullptr) bias_add_diagonals<SUB + 3>(sums + dist, diag);
+      if (near && bias.part != nullptr) bias_add_diagonals<SUB + 3>(sums + dist, diag);
     }
   }
 #pragma unroll
@@ -1236,7 +1284,8 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
   }
   if constexpr (BIAS) {
     if (bias.part != nullptr)
-      bias_store_sums<C::WAVES>(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets, bias, 0.f,
+      bias_store_sums<C::WAVES>(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets, bias,
+                                (far_sum[0] + far_sum[1]) + (far_sum[2] + far_sum[3]),
                                 bias.part + ((int64_t)bh * nqb + qb) * (bias.max_distance + 1));
   }
   if (grad.sq != nullptr) {   // uniform: bias gradient += column sums of dQ over this workgroup's queries
