@@ -102,6 +102,20 @@ typedef struct paci_shapes {
                            them to G before the update or an earlier read of G. Same sum up to fp32
                            rounding order; costs K - 1 more activation slots plus the window's
                            output gradients */
+  /* Positions and norms inside every block's attention (the paper's stages use none of these; all 0
+     is its model). They are the operators of paci_qk_norm_rope_* and paci_attn_* on the block's
+     activations, with the parameters h{l}.q_g, k_g and rel. */
+  int32_t qk_norm;      /* 1: RMS norm of every query and key head (epsilon ln_eps) with gains q_g, k_g
+                           [head_dim], one pair per block; 0: none */
+  int32_t rope_dims;    /* rotated elements of every query and key head, a multiple of 16 up to
+                           head_dim, by the token's position in its sequence; 0: none */
+  float rope_theta;     /* their frequencies are rope_theta^(-2 i / rope_dims) (> 0 when rope_dims > 0) */
+  int32_t rope_pairs;   /* enum paci_rope_pairs */
+  int32_t rel_buckets;  /* relative position bias: rows of each block's table rel [rel_buckets, n_heads], a
+                           multiple of 8 up to 256, with the bounds of paci_rel_bounds; 0: none. A backward
+                           differentiates the probabilities of its forward, so every micro-batch in
+                           flight keeps the tables its forward read, as it keeps its activations */
+  int32_t rel_max_distance; /* rel_buckets / 2 < rel_max_distance <= 512 */
 } paci_shapes;
 
 typedef struct paci_counters {
@@ -162,7 +176,8 @@ int paci_schedule_flush(int M, int K, int delay, int32_t* kinds, int32_t* idx, i
 
 /* ---- parameter layout (host only) ------------------------------------------
  * The canonical order: first stage prefix wte [V, d], wpe [max_pos, d]; per
- * block l: h{l}.ln1_g, ln1_b, w_qkv [3d, d], b_qkv, w_o [d, d], b_o, ln2_g,
+ * block l: h{l}.ln1_g, ln1_b, w_qkv [3d, d], b_qkv, (q_g, k_g [head_dim] with
+ * qk_norm), (rel [rel_buckets, n_heads] with rel_buckets), w_o [d, d], b_o, ln2_g,
  * ln2_b, w_1 [f, d], b_1, w_2 [d, f], b_2; last stage suffix lnf_g, lnf_b,
  * w_lm [V, d]. The flat canonical vector is the concatenation in this order
  * with no padding. Weight decay applies to the w_* matrices only (appendix

@@ -26,6 +26,8 @@ import math
 
 import numpy as np
 
+from . import positions
+
 
 # ----------------------------------------------------------------------------
 # LayerNorm
@@ -177,6 +179,51 @@ def attention_bwd(do_, qkv, lse, mu, S, n_heads, head_dim, keep=None, drop_scale
 
 
 # ----------------------------------------------------------------------------
+# positions inside attention (options of the stage; the paper's uses none)
+# ----------------------------------------------------------------------------
+def _qk_setup(p, cfg):
+    """Gains [2H, dh] or None, positions, frequencies and pairing of the query and key heads."""
+    H = cfg["n_heads"]
+    gain = np.concatenate([np.tile(p["q_g"], (H, 1)), np.tile(p["k_g"], (H, 1))]) if cfg.get("qk_norm") else None
+    R = cfg.get("rope_dims", 0)
+    pos = np.tile(np.arange(cfg["seq"]), cfg["micro_batch"])
+    return gain, pos, positions.freqs(cfg.get("rope_theta", 10000.0), R), cfg.get("rope_pairs", "half")
+
+
+def position_fwd(qkv, p, cfg):
+    """qkv with the query and key heads normalised and rotated, and the bias [H, S] by
+    distance (None without a table) of the attention that reads it."""
+    T, d = qkv.shape[0], cfg["d_model"]
+    bias = None
+    if cfg.get("rel_buckets"):
+        md = cfg["rel_max_distance"]
+        bias = positions.bias_by_distance(p["rel"], positions.bounds(cfg["rel_buckets"], md), md, cfg["seq"])
+    if not (cfg.get("qk_norm") or cfg.get("rope_dims")):
+        return qkv, bias
+    gain, pos, freq, pairs = _qk_setup(p, cfg)
+    qk = positions.norm_rope_fwd(qkv[:, :2 * d].reshape(T, -1, cfg["head_dim"]), gain, pos, freq, pairs, cfg["ln_eps"])
+    return np.concatenate([qk.reshape(T, 2 * d), qkv[:, 2 * d:]], 1), bias
+
+
+def position_bwd(dqkv, ds, qkv, p, cfg):
+    """Backward of position_fwd at the gains of p: (d(qkv), gradients of q_g, k_g and rel).
+    dqkv is the gradient of its result, ds [H, S, S] that of the biased scores."""
+    T, d, H = qkv.shape[0], cfg["d_model"], cfg["n_heads"]
+    g = {}
+    if cfg.get("rel_buckets"):
+        md = cfg["rel_max_distance"]
+        g["rel"] = positions.table_grad(ds, positions.bounds(cfg["rel_buckets"], md), md)
+    if not (cfg.get("qk_norm") or cfg.get("rope_dims")):
+        return dqkv, g
+    gain, pos, freq, pairs = _qk_setup(p, cfg)
+    heads = lambda a: a[:, :2 * d].reshape(T, -1, cfg["head_dim"])  # noqa: E731
+    dqk, dgain = positions.norm_rope_bwd(heads(dqkv), heads(qkv), gain, pos, freq, pairs, cfg["ln_eps"])
+    if dgain is not None:
+        g["q_g"], g["k_g"] = dgain[:H].sum(0), dgain[H:].sum(0)
+    return np.concatenate([dqk.reshape(T, 2 * d), dqkv[:, 2 * d:]], 1), g
+
+
+# ----------------------------------------------------------------------------
 # one pre-LN decoder block
 # ----------------------------------------------------------------------------
 def block_fwd(x, p, cfg, drop=None):
@@ -194,7 +241,8 @@ def block_fwd(x, p, cfg, drop=None):
     sc = 1.0 if drop is None else drop["scale"]
     n1, mean1, rstd1 = layernorm_fwd(x, p["ln1_g"], p["ln1_b"], eps)
     qkv = n1 @ p["w_qkv"].T + p["b_qkv"]
-    o, lse = attention_fwd(qkv, mu, S, H, dh, None if drop is None else drop["attn"], sc)
+    att, bias = position_fwd(qkv, p, cfg)
+    o, lse = attention_fwd(att, mu, S, H, dh, None if drop is None else drop["attn"], sc, bias=bias)
     z1 = o @ p["w_o"].T + p["b_o"]
     x1 = x + (z1 if drop is None else z1 * drop["proj"] * sc)
     n2, mean2, rstd2 = layernorm_fwd(x1, p["ln2_g"], p["ln2_b"], eps)
@@ -203,7 +251,7 @@ def block_fwd(x, p, cfg, drop=None):
     z2 = a @ p["w_2"].T + p["b_2"]
     y = x1 + (z2 if drop is None else z2 * drop["ffn"] * sc)
     saved = dict(x=x, mean1=mean1, rstd1=rstd1, n1=n1, qkv=qkv, o=o, lse=lse,
-                 x1=x1, mean2=mean2, rstd2=rstd2, n2=n2, u=u, a=a, drop=drop)
+                 x1=x1, mean2=mean2, rstd2=rstd2, n2=n2, u=u, a=a, drop=drop, att=att, bias=bias)
     return y, saved
 
 
@@ -234,8 +282,12 @@ def block_bwd(dy, s, p, cfg):
     g["w_o"] = g1.T @ s["o"]
     g["b_o"] = g1.sum(axis=0)
     do_ = g1 @ p["w_o"]
-    dqkv = attention_bwd(do_, s["qkv"], s["lse"], mu, S, H, dh, None if drop is None else drop["attn"],
-                         1.0 if drop is None else drop["scale"])
+    # the probabilities are the forward's: its att, lse and bias (saved), whatever the table is now
+    datt = attention_bwd(do_, s["att"], s["lse"], mu, S, H, dh, None if drop is None else drop["attn"],
+                         1.0 if drop is None else drop["scale"], bias=s["bias"])
+    datt, ds = datt if s["bias"] is not None else (datt, None)
+    dqkv, extra = position_bwd(datt, ds, s["qkv"], p, cfg)
+    g.update(extra)
     # qkv = n1 Wqkv^T + bqkv
     g["w_qkv"] = dqkv.T @ s["n1"]
     g["b_qkv"] = dqkv.sum(axis=0)

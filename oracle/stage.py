@@ -25,6 +25,8 @@ Parameter naming and order (nn.Linear weights are [out, in]):
   block l             h{l}.ln1_g, h{l}.ln1_b, h{l}.w_qkv [3d, d], h{l}.b_qkv,
                       h{l}.w_o [d, d], h{l}.b_o, h{l}.ln2_g, h{l}.ln2_b,
                       h{l}.w_1 [f, d], h{l}.b_1, h{l}.w_2 [d, f], h{l}.b_2
+                      (after b_qkv: q_g, k_g [head_dim] with cfg["qk_norm"], rel
+                      [rel_buckets, n_heads] with cfg["rel_buckets"])
   last stage suffix   lnf_g, lnf_b, w_lm [V, d]
 Weight decay applies to the w_* matrices only (no decay on biases, LayerNorm
 parameters or embeddings, appendix "Detailed experimental setup").
@@ -38,6 +40,13 @@ BLOCK_PARAMS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o",
                 "ln2_g", "ln2_b", "w_1", "b_1", "w_2", "b_2")
 
 
+def block_params(cfg):
+    """Names of a block's parameters in order, the optional ones of its attention included."""
+    extra = (("q_g", "k_g") if cfg.get("qk_norm") else ()) + (("rel",) if cfg.get("rel_buckets") else ())
+    at = BLOCK_PARAMS.index("b_qkv") + 1
+    return BLOCK_PARAMS[:at] + extra + BLOCK_PARAMS[at:]
+
+
 def param_shapes(cfg):
     """Ordered (name, shape) list of a stage's parameters."""
     d, f, V, P = cfg["d_model"], cfg["d_ff"], cfg.get("vocab", 0), cfg.get("max_pos", 0)
@@ -46,9 +55,10 @@ def param_shapes(cfg):
         out += [("wte", (V, d)), ("wpe", (P, d))]
     per = {"ln1_g": (d,), "ln1_b": (d,), "w_qkv": (3 * d, d), "b_qkv": (3 * d,),
            "w_o": (d, d), "b_o": (d,), "ln2_g": (d,), "ln2_b": (d,),
-           "w_1": (f, d), "b_1": (f,), "w_2": (d, f), "b_2": (d,)}
+           "w_1": (f, d), "b_1": (f,), "w_2": (d, f), "b_2": (d,), "q_g": (cfg["head_dim"],), "k_g": (cfg["head_dim"],),
+           "rel": (cfg.get("rel_buckets", 0), cfg["n_heads"])}
     for l in range(cfg["n_layers"]):
-        out += [(f"h{l}.{n}", per[n]) for n in BLOCK_PARAMS]
+        out += [(f"h{l}.{n}", per[n]) for n in block_params(cfg)]
     if cfg["kind"] == "last":
         out += [("lnf_g", (d,)), ("lnf_b", (d,)), ("w_lm", (V, d))]
     return out
@@ -91,7 +101,7 @@ def stage_fwd(cfg, theta, inp, targets=None, mb=0):
     else:
         x = inp
     for l in range(cfg["n_layers"]):
-        p = {n: theta[f"h{l}.{n}"] for n in BLOCK_PARAMS}
+        p = {n: theta[f"h{l}.{n}"] for n in block_params(cfg)}
         x, s = model.block_fwd(x, p, cfg, _drop_masks(cfg, mb, l))
         saved["blocks"].append(s)
     if cfg["kind"] == "last":
@@ -117,7 +127,7 @@ def stage_bwd(cfg, theta, saved, grad_out, K, ids=None):
     else:
         dy = grad_out
     for l in reversed(range(cfg["n_layers"])):
-        p = {n: theta[f"h{l}.{n}"] for n in BLOCK_PARAMS}
+        p = {n: theta[f"h{l}.{n}"] for n in block_params(cfg)}
         dy, gl = model.block_bwd(dy, saved["blocks"][l], p, cfg)
         for n, v in gl.items():
             g[f"h{l}.{n}"] = v

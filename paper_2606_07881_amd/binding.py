@@ -31,6 +31,7 @@ FP32, BF16 = 0, 1
 PARAMS, GRADS, EXP_AVG, EXP_AVG_SQ = 0, 1, 2, 3
 KINDS = {"middle": MIDDLE, "first": FIRST, "last": LAST}
 DTYPES = {"fp32": FP32, "bf16": BF16}
+ROPE_PAIRS = {"half": 0, "adjacent": 1}
 
 
 class PaciShapes(ctypes.Structure):
@@ -39,7 +40,9 @@ class PaciShapes(ctypes.Structure):
                [(n, ctypes.c_float) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "ln_eps")] + \
                [("recompute", ctypes.c_int32), ("lr_warmup", ctypes.c_int32), ("lr_total", ctypes.c_int32),
                 ("lr_min_ratio", ctypes.c_float), ("fused_head", ctypes.c_int32), ("dropout", ctypes.c_float),
-                ("dropout_seed", ctypes.c_uint32), ("window", ctypes.c_int32)]
+                ("dropout_seed", ctypes.c_uint32), ("window", ctypes.c_int32), ("qk_norm", ctypes.c_int32),
+                ("rope_dims", ctypes.c_int32), ("rope_theta", ctypes.c_float), ("rope_pairs", ctypes.c_int32),
+                ("rel_buckets", ctypes.c_int32), ("rel_max_distance", ctypes.c_int32)]
 
 
 class PaciCounters(ctypes.Structure):
@@ -170,6 +173,12 @@ def shapes(cfg):
     s.dropout = float(cfg.get("dropout", 0.0))
     s.dropout_seed = int(cfg.get("dropout_seed", 0)) & 0xFFFFFFFF
     s.window = int(bool(cfg.get("window", False)))
+    s.qk_norm = int(bool(cfg.get("qk_norm", False)))
+    s.rope_dims = int(cfg.get("rope_dims", 0))
+    s.rope_theta = float(cfg.get("rope_theta", 10000.0))
+    s.rope_pairs = ROPE_PAIRS[cfg.get("rope_pairs", "half")]
+    s.rel_buckets = int(cfg.get("rel_buckets", 0))
+    s.rel_max_distance = int(cfg.get("rel_max_distance", 0))
     return s
 
 
@@ -417,7 +426,6 @@ class Stage:
 # [rows, columns] with contiguous rows (any row stride the C ABI admits, e.g. a
 # column range of a fused projection); vectors are contiguous.
 _TORCH_DTYPES = {torch.bfloat16: BF16, torch.float32: FP32}
-ROPE_PAIRS = {"half": 0, "adjacent": 1}
 
 
 def rope_freqs(theta, rope_dims):

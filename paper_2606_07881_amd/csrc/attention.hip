@@ -1418,7 +1418,7 @@ int dq_blocks(const AttnArgs& a) {
 
 template <typename T, int DH>
 hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, const void* dO, const float* lse2, float* ws,
-                      hipStream_t st) {
+                      float* bias_ws, hipStream_t st) {
   const int mu = a.mu, S = a.S, H = a.H, d = H * DH;
   const float scale = 1.f / sqrtf((float)DH);
   const float scale_log2 = LOG2E * scale;
@@ -1426,7 +1426,7 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
   const GradView<T> grad{reinterpret_cast<T*>(gr.dq), reinterpret_cast<T*>(gr.dk), reinterpret_cast<T*>(gr.dv), gr.ldq, gr.ldk,
                          gr.ldv, gr.sum_q, gr.sum_k, gr.sum_v};
   BiasArgs ba = bias_args(a);
-  if (a.table && gr.g_table) ba.part = ws + attn_bwd_workspace_floats(a.dt, mu, S, H);
+  if (a.table && gr.g_table) ba.part = bias_ws;
   const int64_t rows = (int64_t)mu * S * H;
   auto launch = [&](auto bias) {
     constexpr bool B = decltype(bias)::value;
@@ -1514,16 +1514,16 @@ int64_t attn_bias_workspace_floats(const AttnArgs& a) {
 }
 
 hipError_t attn_bwd(const AttnArgs& a, const AttnGrads& g, const void* o, const void* dO, const float* lse2, float* ws,
-                    hipStream_t st) {
+                    float* bias_ws, hipStream_t st) {
   if (!attn_args_ok(a)) return hipErrorInvalidValue;
   if (a.dt == DT_BF16) {
-    if (a.dh == 32) return bwd_launch<bf16, 32>(a, g, o, dO, lse2, ws, st);
-    if (a.dh == 64) return bwd_launch<bf16, 64>(a, g, o, dO, lse2, ws, st);
-    if (a.dh == 128) return bwd_launch<bf16, 128>(a, g, o, dO, lse2, ws, st);
+    if (a.dh == 32) return bwd_launch<bf16, 32>(a, g, o, dO, lse2, ws, bias_ws, st);
+    if (a.dh == 64) return bwd_launch<bf16, 64>(a, g, o, dO, lse2, ws, bias_ws, st);
+    if (a.dh == 128) return bwd_launch<bf16, 128>(a, g, o, dO, lse2, ws, bias_ws, st);
     return hipErrorInvalidValue;
   }
-  if (a.dh == 32) return bwd_launch<float, 32>(a, g, o, dO, lse2, ws, st);
-  if (a.dh == 64) return bwd_launch<float, 64>(a, g, o, dO, lse2, ws, st);
+  if (a.dh == 32) return bwd_launch<float, 32>(a, g, o, dO, lse2, ws, bias_ws, st);
+  if (a.dh == 64) return bwd_launch<float, 64>(a, g, o, dO, lse2, ws, bias_ws, st);
   return hipErrorInvalidValue;
 }
 

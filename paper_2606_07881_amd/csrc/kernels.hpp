@@ -195,11 +195,11 @@ struct AttnGrads {
 // log2 units. A query with no key left has o = 0 and lse2 = -inf.
 hipError_t attn_fwd(const AttnArgs& a, void* o, float* lse2, hipStream_t st);
 // Backward: D = rowsum(dO * O) per (b, h, query), then dK, dV and dQ. ws is workspace of
-// attn_bwd_workspace_floats() floats, followed by attn_bias_workspace_floats() for g_table.
+// attn_bwd_workspace_floats() floats, bias_ws of attn_bias_workspace_floats() (g_table only).
 int64_t attn_bwd_workspace_floats(DType dt, int mu, int S, int H);
 int64_t attn_bias_workspace_floats(const AttnArgs& a);   // reads dt, mu, S, H, dh, max_distance
 hipError_t attn_bwd(const AttnArgs& a, const AttnGrads& g, const void* o, const void* dO, const float* lse2, float* ws,
-                    hipStream_t st);
+                    float* bias_ws, hipStream_t st);
 
 // ---- LayerNorm -----------------------------------------------------------------------
 // n = (x - mean) * rstd * gamma + beta, per row of d; xcopy (optional) receives x.

@@ -256,6 +256,7 @@ extern "C" int paci_attn_backward(const paci_attn_shapes* s, const void* dev_q, 
   g.dv = dev_dv;
   g.ldv = ld_dv;
   g.g_table = dev_g_table;
-  return done(paci::attn_bwd(a, g, dev_o, dev_do, dev_lse2, reinterpret_cast<float*>(dev_ws),
+  float* ws = reinterpret_cast<float*>(dev_ws);
+  return done(paci::attn_bwd(a, g, dev_o, dev_do, dev_lse2, ws, ws + paci::attn_bwd_workspace_floats(a.dt, a.mu, a.S, a.H),
                              reinterpret_cast<hipStream_t>(hip_stream)));
 }

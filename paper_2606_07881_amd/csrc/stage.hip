@@ -216,6 +216,7 @@ struct TensorRef {
 
 struct BlockRefs {
   int64_t ln1_g, ln1_b, w_qkv, b_qkv, w_o, b_o, ln2_g, ln2_b, w_1, b_1, w_2, b_2;
+  int64_t q_g = -1, k_g = -1, rel = -1;   // optional
 };
 
 struct ParamTable {
@@ -269,6 +270,13 @@ int validate_shapes(const paci_shapes* s, int K, int delay) {
   if (T > (1LL << 30)) return PACI_E_UNSUPPORTED;
   if (s->window && (s->recompute || s->dtype != PACI_BF16 || T % 64 || s->d_model % 8 || s->d_ff % 8))
     return PACI_E_UNSUPPORTED;   // the windowed contraction: stored bf16 activations in 64-row segments
+  if ((s->qk_norm != 0 && s->qk_norm != 1) || s->rope_dims < 0 || s->rope_dims > dh || s->rel_buckets < 0) return PACI_E_INVAL;
+  if (s->rope_dims && (!(s->rope_theta > 0.f) || !std::isfinite(s->rope_theta))) return PACI_E_INVAL;
+  if (s->rope_pairs != PACI_ROPE_HALF && s->rope_pairs != PACI_ROPE_ADJACENT) return PACI_E_INVAL;
+  if (s->rel_buckets && s->rel_max_distance <= s->rel_buckets / 2) return PACI_E_INVAL;
+  if (s->rope_dims % 16 || s->rel_buckets % 8) return PACI_E_UNSUPPORTED;
+  if (s->rel_buckets && (s->rel_buckets > paci::MAX_BUCKETS || s->rel_max_distance > paci::MAX_DISTANCE))
+    return PACI_E_UNSUPPORTED;
   return PACI_OK;
 }
 
@@ -286,6 +294,11 @@ ParamTable build_params(const paci_shapes& s) {
     b.ln1_b = p.add(h + "ln1_b", d, 1, false);
     b.w_qkv = p.add(h + "w_qkv", 3 * d, d, true);
     b.b_qkv = p.add(h + "b_qkv", 3 * d, 1, false);
+    if (s.qk_norm) {
+      b.q_g = p.add(h + "q_g", s.head_dim, 1, false);
+      b.k_g = p.add(h + "k_g", s.head_dim, 1, false);
+    }
+    if (s.rel_buckets) b.rel = p.add(h + "rel", s.rel_buckets, s.n_heads, false);
     b.w_o = p.add(h + "w_o", d, d, true);
     b.b_o = p.add(h + "b_o", d, 1, false);
     b.ln2_g = p.add(h + "ln2_g", d, 1, false);
@@ -317,6 +330,7 @@ struct Bump {
 
 struct BlockSlot {  // byte offsets inside one activation slot
   size_t x, n1, qkv, o, x1, n2, gu, a, mean1, rstd1, mean2, rstd2, lse2;   // gu = gelu'(u), a = gelu(u)
+  size_t qk = 0, rel = 0;   // normalised and rotated q and k [T, 2d]; the forward's bias table
 };
 
 struct Layout {
@@ -326,6 +340,10 @@ struct Layout {
   size_t theta, G, m, v, theta16, theta16T = 0, chunks, zeros, ctl = 0, guard = 0;
   bool wT = false;             // transposed bf16 block weights kept (theta16T)
   int nchunks = 0, nguard = 0;
+  // norms and rotation of q and k, relative position bias
+  bool rot = false, rel = false;
+  size_t freq = 0, bounds = 0;    // fp64 frequencies, int32 bounds (written at init)
+  size_t w_rot = 0, w_bias = 0;   // workspaces of their backwards
   size_t stash, slot_bytes;
   int n_slots = 1;             // activation slots: delay + 1, or K + delay with windowed weight gradients
   bool window = false;         // weight gradients windowed over the K micro-batches of a window
@@ -402,6 +420,21 @@ std::vector<int2> guard_table(const ParamTable& p) {
   return v;
 }
 
+// The norms and rotation of a block's query and key heads, pointers unset.
+paci::RotArgs rot_args(const paci_shapes& s) {
+  paci::RotArgs r;
+  r.dt = s.dtype == PACI_BF16 ? paci::DT_BF16 : paci::DT_F32;
+  r.T = s.micro_batch * s.seq;
+  r.seq = s.seq;
+  r.q_heads = r.k_heads = s.n_heads;
+  r.dh = s.head_dim;
+  r.rope_dims = s.rope_dims;
+  r.norm = s.qk_norm != 0;
+  r.adjacent = s.rope_pairs == PACI_ROPE_ADJACENT;
+  r.eps = s.ln_eps;
+  return r;
+}
+
 Layout make_layout(const paci_shapes& s, int K, int delay, const ParamTable& p) {
   Layout L;
   const int64_t esz = s.dtype == PACI_BF16 ? 2 : 4;
@@ -426,6 +459,10 @@ Layout make_layout(const paci_shapes& s, int K, int delay, const ParamTable& p) 
   L.nguard = (int)guard_table(p).size();
   L.guard = a.take(8 * (size_t)std::max(1, L.nguard));
   L.zeros = a.take(256);  // never written after init: source of out-of-range GEMM tile slots
+  L.rot = s.qk_norm || s.rope_dims;
+  L.rel = s.rel_buckets > 0;
+  if (s.rope_dims) L.freq = a.take(8 * (size_t)(s.rope_dims / 2));
+  if (L.rel) L.bounds = a.take(4 * (size_t)s.rel_buckets);
   L.ctl = a.take(256);    // update control: {G not finite, updates applied, updates skipped, 0}
 
   // one activation slot
@@ -445,6 +482,8 @@ Layout make_layout(const paci_shapes& s, int K, int delay, const ParamTable& p) 
     b.mean2 = sl.take(4 * T);
     b.rstd2 = sl.take(4 * T);
     b.lse2 = sl.take(4 * heads_rows);
+    if (L.rot) b.qk = sl.take(esz * T * 2 * d);
+    if (L.rel) b.rel = sl.take(4 * (size_t)s.rel_buckets * s.n_heads);
     L.blk.push_back(b);
   }
   if (s.kind == PACI_FIRST) L.s_ids = sl.take(4 * T);
@@ -515,6 +554,17 @@ Layout make_layout(const paci_shapes& s, int K, int delay, const ParamTable& p) 
   L.w_dqkv = a.take(esz * T * 3 * d);
   L.w_D = a.take(4 * (size_t)paci::attn_bwd_workspace_floats(s.dtype == PACI_BF16 ? paci::DT_BF16 : paci::DT_F32,
                                                               s.micro_batch, s.seq, s.n_heads));
+  if (L.rot) L.w_rot = a.take(4 * (size_t)paci::rotary_workspace_floats(rot_args(s)));
+  if (L.rel) {
+    paci::AttnArgs aa;
+    aa.dt = s.dtype == PACI_BF16 ? paci::DT_BF16 : paci::DT_F32;
+    aa.mu = s.micro_batch;
+    aa.S = s.seq;
+    aa.H = s.n_heads;
+    aa.dh = s.head_dim;
+    aa.max_distance = s.rel_max_distance;
+    L.w_bias = a.take(4 * (size_t)paci::attn_bias_workspace_floats(aa));
+  }
   int64_t part = 64;
   if (s.kind == PACI_LAST) {
     part = std::max(part, paci::ce_part_floats((int)T));
@@ -542,11 +592,11 @@ Layout make_layout(const paci_shapes& s, int K, int delay, const ParamTable& p) 
 // ---- kernel timing families -------------------------------------------------------------------
 enum Family {
   F_GEMM_FWD = 0, F_GEMM_DGRAD, F_GEMM_WGRAD, F_ATTN_FWD, F_ATTN_BWD, F_LN_FWD, F_LN_BWD, F_BIAS_GRAD, F_ADAMW,
-  F_EMBED, F_CE, F_COPY, F_DROPOUT, F_COUNT
+  F_EMBED, F_CE, F_COPY, F_DROPOUT, F_ROTARY, F_COUNT
 };
 const char* kFamilyNames[F_COUNT] = {"gemm_fwd", "gemm_dgrad", "gemm_wgrad_acc", "attn_fwd", "attn_bwd",
                                      "layernorm_fwd", "layernorm_bwd", "bias_grad", "adamw", "embedding",
-                                     "cross_entropy", "copy", "dropout"};
+                                     "cross_entropy", "copy", "dropout", "qk_norm_rope"};
 
 }  // namespace
 
@@ -771,12 +821,57 @@ paci::AttnArgs attn_args(const paci_stage* h, const char* sl, int l, int mb) {
   a.S = s.seq;
   a.H = s.n_heads;
   a.dh = s.head_dim;
-  a.q = sl + h->L.blk[l].qkv;
-  a.k = sl + h->L.blk[l].qkv + d * h->esz;
+  const bool rot = h->L.rot;   // then q and k lie in a buffer of their own
+  a.q = sl + (rot ? h->L.blk[l].qk : h->L.blk[l].qkv);
+  a.k = reinterpret_cast<const char*>(a.q) + d * h->esz;
   a.v = sl + h->L.blk[l].qkv + 2 * d * h->esz;
-  a.ldq = a.ldk = a.ldv = 3 * (int64_t)d;
+  a.ldq = a.ldk = (rot ? 2 : 3) * (int64_t)d;
+  a.ldv = 3 * (int64_t)d;
+  if (h->L.rel) {
+    a.table = reinterpret_cast<const float*>(sl + h->L.blk[l].rel);
+    a.bounds = reinterpret_cast<const int32_t*>(h->arena + h->L.bounds);
+    a.n_buckets = s.rel_buckets;
+    a.max_distance = s.rel_max_distance;
+  }
   a.drop = h->drop(mb, l, SITE_ATTN);
   return a;
+}
+
+// Forward: q and k of block l normalised and rotated, from the projection into the
+// activation area. Backward: in place on the q and k columns of dqkv, with the gains
+// current now; G of the gains and of the projection's q and k biases.
+paci::RotArgs block_rot(const paci_stage* h, const char* sl, int l) {
+  const BlockRefs& b = h->p.blocks[l];
+  paci::RotArgs r = rot_args(h->s);
+  r.x = sl + h->L.blk[l].qkv;
+  r.ldx = 3 * (int64_t)h->s.d_model;
+  if (r.norm) {
+    r.gain_q = h->th(b.q_g);
+    r.gain_k = h->th(b.k_g);
+  }
+  r.freq = reinterpret_cast<const double*>(h->arena + h->L.freq);
+  return r;
+}
+int rotary_fwd(paci_stage* h, char* sl, int l) {
+  const int64_t d = h->s.d_model;
+  paci::RotArgs r = block_rot(h, sl, l);
+  r.out = sl + h->L.blk[l].qk;
+  r.ldout = 2 * d;
+  return run(h, F_ROTARY, 4.0 * h->L.T * d * h->esz, [&] { return paci::rotary(r, false, h->st); });
+}
+int rotary_bwd(paci_stage* h, const char* sl, int l, char* dqkv) {
+  const BlockRefs& b = h->p.blocks[l];
+  const int64_t d = h->s.d_model;
+  paci::RotArgs r = block_rot(h, sl, l);
+  r.dy = r.out = dqkv;
+  r.lddy = r.ldout = 3 * d;
+  if (r.norm) {
+    r.g_gain_q = h->g(b.q_g);
+    r.g_gain_k = h->g(b.k_g);
+  }
+  r.g_bias = h->g(b.b_qkv);
+  r.ws = reinterpret_cast<float*>(h->ws(h->L.w_rot));
+  return run(h, F_ROTARY, (r.norm ? 6.0 : 4.0) * h->L.T * d * h->esz, [&] { return paci::rotary(r, true, h->st); });
 }
 
 // ---- forward of the block stack -----------------------------------------------------------------
@@ -793,6 +888,13 @@ int blocks_fwd(paci_stage* h, char* sl, const void* in, void* x0_copy, void* out
     float* rstd1 = reinterpret_cast<float*>(sl + o.rstd1);
     TRY(ln_fwd(h, x, sl + o.n1, mean1, rstd1, b.ln1_g, b.ln1_b, l == 0 ? x0_copy : nullptr));
     TRY(linear_fwd(h, sl + o.n1, b.w_qkv, b.b_qkv, T, 3 * d, d, paci::EPI_BIAS, sl + o.qkv, nullptr, nullptr));
+    if (h->L.rot) TRY(rotary_fwd(h, sl, l));
+    if (h->L.rel) {
+      const size_t bytes = 4 * (size_t)s.rel_buckets * s.n_heads;
+      TRY(run(h, F_COPY, 2.0 * bytes, [&] {
+        return hipMemcpyAsync(sl + o.rel, h->th(b.rel), bytes, hipMemcpyDeviceToDevice, h->st);
+      }));
+    }
     TRY(run(h, F_ATTN_FWD, 4.0 * attn_pairs(s) * s.head_dim, [&] {
       return paci::attn_fwd(attn_args(h, sl, l, mb), sl + o.o, reinterpret_cast<float*>(sl + o.lse2), h->st);
     }));
@@ -877,12 +979,16 @@ int block_bwd(paci_stage* h, char* sl, int l, const void* dy, void* dx, bool dy_
     gr.dk = dqkv + (size_t)d * h->esz;
     gr.dv = dqkv + 2 * (size_t)d * h->esz;
     gr.ldq = gr.ldk = gr.ldv = 3 * d;
-    gr.sum_q = h->g(b.b_qkv);
-    gr.sum_k = gr.sum_q + d;
-    gr.sum_v = gr.sum_k + d;
+    gr.sum_v = h->g(b.b_qkv) + 2 * d;
+    if (!L.rot) {   // else the rotation's backward sums what it makes of dq and dk
+      gr.sum_q = h->g(b.b_qkv);
+      gr.sum_k = gr.sum_q + d;
+    }
+    if (L.rel) gr.g_table = h->g(b.rel);
     return paci::attn_bwd(attn_args(h, sl, l, mb), gr, sl + o.o, dO, reinterpret_cast<const float*>(sl + o.lse2), h->pairs,
-                          h->st);
+                          reinterpret_cast<float*>(h->ws(L.w_bias)), h->st);
   }));
+  if (L.rot) TRY(rotary_bwd(h, sl, l, dqkv));
   // qkv = n1 Wqkv^T + bqkv
   if (!win) TRY(linear_wgrad(h, dqkv, 3 * d, sl + o.n1, d, 3 * d, d, T, b.w_qkv));
   TRY(linear_dgrad(h, dqkv, 3 * d, b.w_qkv, T, d, 3 * d, paci::EPI_STORE, dn, nullptr));
@@ -1145,6 +1251,14 @@ extern "C" int paci_stage_init(const paci_shapes* s, int K, int delay, void* dev
   if (e == hipSuccess && !granges.empty())
     e = hipMemcpyAsync(h->arena + h->L.guard, granges.data(), granges.size() * sizeof(int2), hipMemcpyHostToDevice,
                        h->st);
+  std::vector<double> freq(s->rope_dims / 2);
+  if (s->rope_dims) (void)paci_rope_freqs(s->rope_theta, s->rope_dims, freq.data());
+  if (e == hipSuccess && s->rope_dims)
+    e = hipMemcpyAsync(h->arena + h->L.freq, freq.data(), freq.size() * sizeof(double), hipMemcpyHostToDevice, h->st);
+  std::vector<int32_t> bounds(s->rel_buckets);
+  if (h->L.rel) (void)paci_rel_bounds(s->rel_buckets, s->rel_max_distance, bounds.data());
+  if (e == hipSuccess && h->L.rel)
+    e = hipMemcpyAsync(h->arena + h->L.bounds, bounds.data(), bounds.size() * sizeof(int32_t), hipMemcpyHostToDevice, h->st);
   std::vector<paci::WgradProblem> tabs;
   if (h->L.wdefer) tabs = wgrad_tables(h);
   if (e == hipSuccess && !tabs.empty())

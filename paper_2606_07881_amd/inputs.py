@@ -7,7 +7,8 @@ own and both sides of a parity check see identical bits.
 
 Recipe (the paper's GPT-2 Medium pretraining on OpenWebText is replaced by
 synthetic data with these distributions):
-  weights and embeddings ~ N(0, 0.02^2), biases 0, LayerNorm gamma 1, beta 0;
+  weights and embeddings ~ N(0, 0.02^2), biases 0, LayerNorm gamma 1, beta 0
+  (query and key gains 1, relative position tables ~ N(0, 0.02^2));
   stage input activations ~ N(0, 1); output gradients ~ N(0, 0.01^2);
   token ids and targets i.i.d. uniform on [0, vocab).
 Normals are drawn in float32. For bf16 stages the activations and gradients
@@ -49,8 +50,12 @@ def param_specs(c):
         out += [("wte", (V, d), "normal"), ("wpe", (P, d), "normal")]
     for l in range(c["n_layers"]):
         out += [(f"h{l}.ln1_g", (d,), "ones"), (f"h{l}.ln1_b", (d,), "zeros"),
-                (f"h{l}.w_qkv", (3 * d, d), "normal"), (f"h{l}.b_qkv", (3 * d,), "zeros"),
-                (f"h{l}.w_o", (d, d), "normal"), (f"h{l}.b_o", (d,), "zeros"),
+                (f"h{l}.w_qkv", (3 * d, d), "normal"), (f"h{l}.b_qkv", (3 * d,), "zeros")]
+        if c.get("qk_norm"):
+            out += [(f"h{l}.q_g", (c["head_dim"],), "ones"), (f"h{l}.k_g", (c["head_dim"],), "ones")]
+        if c.get("rel_buckets"):
+            out += [(f"h{l}.rel", (c["rel_buckets"], c["n_heads"]), "normal")]
+        out += [(f"h{l}.w_o", (d, d), "normal"), (f"h{l}.b_o", (d,), "zeros"),
                 (f"h{l}.ln2_g", (d,), "ones"), (f"h{l}.ln2_b", (d,), "zeros"),
                 (f"h{l}.w_1", (f, d), "normal"), (f"h{l}.b_1", (f,), "zeros"),
                 (f"h{l}.w_2", (d, f), "normal"), (f"h{l}.b_2", (d,), "zeros")]

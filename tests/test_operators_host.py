@@ -152,3 +152,39 @@ def test_binding_refuses_what_it_cannot_pass_on():
         with pytest.raises(binding.PaciError) as e:
             call()
         assert e.value.code == INVAL   # host tensors
+
+
+# ---- the same as options of a stage -------------------------------------------------------
+def test_stage_options_are_checked_and_listed():
+    from oracle import stage as ostage
+    from paper_2606_07881_amd import configs, inputs
+    c = configs.get("gpt2m_mid_bf16", qk_norm=1, rope_dims=64, rel_buckets=32, rel_max_distance=128)
+    out = ctypes.c_size_t(0)
+
+    def arena(**over):
+        s = binding.shapes(dict(c, **{k: v for k, v in over.items() if k != "raw"}))
+        for k, v in over.get("raw", {}).items():
+            setattr(s, k, v)
+        return lib.paci_stage_arena_bytes(ctypes.byref(s), 8, 3, ctypes.byref(out))
+    assert arena() == 0
+    with_options = out.value
+    for over, code in [(dict(raw=dict(qk_norm=2)), INVAL), (dict(rope_dims=-16), INVAL), (dict(rope_dims=80), INVAL),
+                       (dict(rope_dims=8), UNSUP), (dict(rope_theta=0.0), INVAL), (dict(rope_theta=float("nan")), INVAL),
+                       (dict(raw=dict(rope_pairs=2)), INVAL), (dict(rel_buckets=-8), INVAL), (dict(rel_buckets=12), UNSUP),
+                       (dict(rel_max_distance=16), INVAL), (dict(rel_max_distance=513), UNSUP),
+                       (dict(rel_buckets=264, rel_max_distance=512), UNSUP)]:
+        assert arena(**over) == code, over
+    table = binding.param_table(c)
+    specs = inputs.param_specs(c)
+    assert [t["name"] for t in table] == [n for n, _, _ in specs] == [n for n, _ in ostage.param_shapes(c)]
+    names = [t["name"] for t in table][:8]
+    assert names == ["h0.ln1_g", "h0.ln1_b", "h0.w_qkv", "h0.b_qkv", "h0.q_g", "h0.k_g", "h0.rel", "h0.w_o"]
+    off = 0
+    for t, (n, shape, _) in zip(table, specs):
+        assert t["offset"] == off and t["numel"] == int(np.prod(shape)) and t["decay"] == ostage.decayed(n)
+        off += t["numel"]
+    # the normalised q and k of every block and micro-batch in flight, and little else
+    T, d = 8192, 1024
+    assert arena(qk_norm=0, rope_dims=0, rel_buckets=0) == 0
+    extra = with_options - out.value
+    assert 4 * 6 * T * 2 * d * 2 <= extra <= 4 * 6 * T * 2 * d * 2 + (24 << 20)

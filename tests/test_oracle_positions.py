@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import model, positions
+from oracle import model, positions, stage
 
 
 def _rotary_case(pairs, norm, seed=0):
@@ -111,3 +111,41 @@ def test_biased_attention_gradients_match_central_differences():
             b = f()
             arr[ix] = old
             assert abs((a - b) / (2 * h) - grad[ix]) < 1e-7, ix
+
+
+POSITION_CFG = dict(n_layers=2, d_model=8, n_heads=2, head_dim=4, d_ff=32, seq=5, micro_batch=2, vocab=11, max_pos=7,
+                    ln_eps=1e-5, qk_norm=1, rope_dims=4, rope_theta=50.0, rel_buckets=4, rel_max_distance=4)
+
+
+@pytest.mark.parametrize("kind", ["middle", "first", "last"])
+@pytest.mark.parametrize("over", [{}, dict(rope_pairs="adjacent"), dict(qk_norm=0), dict(rope_dims=0), dict(rel_buckets=0)],
+                         ids=str)
+def test_stage_gradients_match_central_differences(kind, over):
+    """The whole stage function with its position options, every parameter."""
+    cfg = dict(POSITION_CFG, kind=kind, **over)
+    g = np.random.default_rng(5)
+    theta = {n: (1 + 0.2 * g.standard_normal(s)) if n.endswith("_g") else 0.3 * g.standard_normal(s)
+             for n, s in stage.param_shapes(cfg)}
+    T = cfg["micro_batch"] * cfg["seq"]
+    inp = g.integers(0, 11, (2, 5)) if kind == "first" else g.standard_normal((T, 8))
+    tgt = g.integers(0, 11, (2, 5)) if kind == "last" else None
+    dy = None if kind == "last" else g.standard_normal((T, 8))
+
+    def f():
+        out, _ = stage.stage_fwd(cfg, theta, inp, tgt)
+        return out if kind == "last" else float((out * dy).sum())
+    _, saved = stage.stage_fwd(cfg, theta, inp, tgt)
+    _, grads = stage.stage_bwd(cfg, theta, saved, dy, 1, ids=inp if kind == "first" else None)
+    assert sorted(grads) == sorted(theta)
+    h = 1e-6
+    for name, arr in theta.items():
+        idx = list(np.ndindex(arr.shape))
+        for ix in [idx[i] for i in g.permutation(len(idx))[:12]]:
+            old = arr[ix]
+            arr[ix] = old + h
+            a = f()
+            arr[ix] = old - h
+            b = f()
+            arr[ix] = old
+            fd = (a - b) / (2 * h)
+            assert abs(grads[name][ix] - fd) <= 1e-7 * max(1.0, abs(fd)) + 1e-8, (name, ix)
