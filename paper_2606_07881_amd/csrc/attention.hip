@@ -46,9 +46,11 @@ template <typename T> struct GradView {
 // ---- relative position bias -------------------------------------------------------------
 // The score of query i and key j <= i adds table[bucket(i - j)][h], where distances
 // from max_distance on share the last bucket reached. A workgroup serves one head, so
-// its bias is a vector over the distance, built once in LDS in units of log 2:
-//   vec[FRONT + n] = log2(e) * table[bucket(n)][h],  n = 0 .. max_distance, then the
+// its bias is a vector over the distance, built once in LDS in the units of q . k:
+//   vec[FRONT + n] = sqrt(dh) * table[bucket(n)][h],  n = 0 .. max_distance, then the
 //   value of max_distance up to n = max_distance + TAIL.
+// The products of a tile start from it instead of from zero (the matrix instruction's
+// third operand), so adding it costs no vector instruction.
 // A tile of 16 queries and 16 keys at distance 16 D holds distances 16 D - 15 .. 16 D + 15,
 // so tiles of equal D read the same values, and a block whose distances all reach
 // max_distance reads none: one value serves it (`far`).
@@ -57,14 +59,16 @@ struct BiasArgs {
   const float* table;      // [n_buckets][H]
   const int32_t* bounds;   // first distance of every bucket, ascending
   int n_buckets, max_distance;
-  float* part;             // dQ workgroups: sums of dS by distance, [heads][query blocks][max_distance + 1], or null
+  float* part;             // dQ wavefronts: sums of dS by distance, [heads][wavefront][max_distance + 1], or null
 };
 constexpr int BIAS_FRONT = 80, BIAS_TAIL = 128;   // distances below 0 (masked keys) and above max_distance inside a window
 constexpr float BIAS_MASKED = -1e30f;
 __host__ __device__ __forceinline__ int bias_len(int max_distance) { return BIAS_FRONT + max_distance + BIAS_TAIL; }
-// LDS behind the tiles, floats: the vector, bounds and table column, then (dQ) one vector of sums per wavefront.
-__host__ __device__ __forceinline__ int bias_lds_floats(int max_distance, int n_buckets, int waves) {
-  return (1 + waves) * bias_len(max_distance) + 2 * n_buckets;
+// A dQ wavefront of SUB query tiles moves its diagonal sums through 4 rows of DiagRow floats of LDS.
+template <int SUB> struct DiagRow { static constexpr int N = 16 * (SUB + 5), FLOATS = 4 * N; };
+// LDS behind the tiles, floats: the vector, bounds and table column, then (dQ) the rows of each wavefront.
+__host__ __device__ __forceinline__ int bias_lds_floats(int max_distance, int n_buckets, int diag) {
+  return bias_len(max_distance) + 2 * n_buckets + diag;
 }
 
 // A query whose every key the bias hides has lse2 = -inf; +inf in its place makes every
@@ -74,13 +78,14 @@ template <bool BIAS> __device__ __forceinline__ float query_lse(float lse2) {
 }
 
 // Builds vec for head h (every thread of the workgroup; NTH threads; ends in a barrier).
-template <int NTH> __device__ __forceinline__ void bias_build(float* vec, const BiasArgs& a, int h, int H) {
+template <int NTH, int DH> __device__ __forceinline__ void bias_build(float* vec, const BiasArgs& a, int h, int H) {
   int* bnd = reinterpret_cast<int*>(vec + bias_len(a.max_distance));
   float* col = vec + bias_len(a.max_distance) + a.n_buckets;
   for (int i = threadIdx.x; i < a.n_buckets; i += NTH) {
     const float t = a.table[(int64_t)i * H + h];
     bnd[i] = a.bounds[i];
-    col[i] = t <= BIAS_MASKED ? -INFINITY : t * LOG2E;
+    // entries so large that the product is not finite count as the largest number
+    col[i] = t <= BIAS_MASKED ? -INFINITY : t > 0.f ? fminf(t * sqrtf((float)DH), 3.4028235e38f) : t * sqrtf((float)DH);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < bias_len(a.max_distance); i += NTH) {
@@ -96,79 +101,88 @@ template <int NTH> __device__ __forceinline__ void bias_build(float* vec, const 
   __syncthreads();
 }
 
-// How a block's scores get their bias: none; one value for the whole block (its distances
-// all reach max_distance); or each from the vector.
-using NoBias = std::integral_constant<int, 0>;
-using FarBias = std::integral_constant<int, 1>;
-using VecBias = std::integral_constant<int, 2>;
-// The one value, and the least distance of a block from which it serves: max_distance, or
-// never where adding it to the score first is not the same as adding it to the exponent
-// (a hidden, NaN or huge entry).
+// The value of a block whose distances all reach max_distance, in units of log 2, and the
+// least distance of a block from which it serves: max_distance, or never where adding it to
+// the exponent is not the same as adding it to the score (a hidden, NaN or huge entry).
 struct FarValue {
   float b;
   int from;
 };
-__device__ __forceinline__ FarValue bias_far(const float* vec, int max_distance) {
-  const float b = as_float(__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, vec[BIAS_FRONT + max_distance])));
+__device__ __forceinline__ FarValue bias_far(const float* vec, int max_distance, float scale_log2) {
+  const float b = scale_log2 * as_float(__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, vec[BIAS_FRONT + max_distance])));
   return {b, fabsf(b) <= 1024.f ? max_distance : 0x7fffffff};
 }
 
-// Sums over the diagonals of dS. acc[i][r] of lane (g = l / 16, c = l % 16) holds the
-// sum over a block's tiles with qs - kt = i - 3 (query tile minus key tile) at distance
-// 16 (i - 3) + c - 4 g - r from the block's own. Moving the r-th value by r lanes within
-// the 16 lines the four up (what leaves a row at its start belongs to the window
-// before); the four lane groups then add into the wavefront's vector one after the
-// other, each to addresses of its own, so the order of the sums is fixed.
-// sums: entry of distance qw0 - k0 (the block's own).
-template <int NB> __device__ __forceinline__ void bias_add_diagonals(float* sums, const float (&acc)[NB][4]) {
-  const int l = lane_id(), g = l >> 4, c = l & 15;
-  float win[NB + 1];
-#pragma unroll
-  for (int i = -1; i < NB; ++i) {
-    float u = i >= 0 ? acc[i < 0 ? 0 : i][0] : 0.f;
-    if (i >= 0) {   // lane c takes lane c + r (row_shl)
-      const int k = i < 0 ? 0 : i;
-      u += dpp_shift<0x101>(acc[k][1]) + dpp_shift<0x102>(acc[k][2]) + dpp_shift<0x103>(acc[k][3]);
-    }
-    if (i + 1 < NB) {   // lane c takes lane c + r - 16 of the next window (row_shr 16 - r)
-      const int k = i + 1 < NB ? i + 1 : 0;
-      u += dpp_shift<0x11F>(acc[k][1]) + dpp_shift<0x11E>(acc[k][2]) + dpp_shift<0x11D>(acc[k][3]);
-    }
-    win[i + 1] = u;
-  }
-  float* at = sums + c - 4 * g;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    if (g == q) {
-#pragma unroll
-      for (int i = 0; i <= NB; ++i) lds_add(at + 16 * (i - 4), win[i]);
-    }
-    __builtin_amdgcn_wave_barrier();   // the four groups stay in this order
-  }
-}
+// Sums over the diagonals of dS, for the table's gradient: a dQ wavefront of 16 SUB
+// queries adds up dS by distance and leaves one row of sums per distance in `part`
+// (distances below max_distance; the last entry holds the rest), which a second
+// launch adds by bucket in a fixed order.
+//
+// acc[i][r] of lane (g = l / 16, c = l % 16) is the sum over a block's tiles with
+// qs - kt = i - 3 (query tile minus key tile), at distance D0 + 16 (i - 3) + c - 4 g - r,
+// where D0 = first query - first key of the block. Moving the r-th value by r lanes
+// within the 16 lines the four up (what leaves a row of lanes belongs to the window
+// before). The lane groups' rows, 4 g apart, meet in LDS: six to eight stores and
+// eight loads a block, where adding all four groups into one vector by LDS atomics
+// took 19 us of a 143 us backward (8 x 1024 tokens, 16 heads of 64, max_distance 128),
+// and this about 3.
+// A block holds distances D0 - 63 .. D0 + 16 SUB - 1, and the next block's D0 is 64 less, so
+// the sums of D0 + 1 .. D0 + 64 are complete with this block: lane j stores distance D0 + 1 + j,
+// this block's part added to what the block before left there (carry).
+template <int SUB> struct DiagSums {
+  static constexpr int NB = SUB + 3, N = DiagRow<SUB>::N;
+  float* rows;       // this wavefront's rows in LDS
+  float* out;        // its row of part, or null
+  int max_distance;
+  float carry = 0.f, far = 0.f;   // sums of the block before; of distances from max_distance on
 
-// The workgroup's sums by distance out to part (WAVES vectors behind one another;
-// far: each lane's sum over blocks beyond max_distance).
-template <int WAVES> __device__ __forceinline__ void bias_store_sums(float* sums, const BiasArgs& a, float far, float* out) {
-  const int len = bias_len(a.max_distance), w = threadIdx.x >> 6;
-  far = wave_sum(far);
-  if (lane_id() == 0) sums[w * len + BIAS_FRONT + a.max_distance] += far;
-  __syncthreads();
-  for (int n = threadIdx.x; n < a.max_distance; n += WAVES * 64) {
-    float s = 0.f;
-#pragma unroll
-    for (int u = 0; u < WAVES; ++u) s += sums[u * len + BIAS_FRONT + n];
-    out[n] = s;
+  __device__ __forceinline__ void init(float* lds, float* to, int md) {
+    rows = lds + (threadIdx.x >> 6) * DiagRow<SUB>::FLOATS;
+    out = to;
+    max_distance = md;
+    // the last 16 entries of a row stay zero (no tile reaches those distances)
+    rows[(lane_id() >> 4) * N + N - 16 + (lane_id() & 15)] = 0.f;
   }
-  if (w == 0) {   // max_distance and beyond
-    float s = 0.f;
-    for (int n = a.max_distance + lane_id(); n < a.max_distance + BIAS_TAIL; n += 64)
-#pragma unroll
-      for (int u = 0; u < WAVES; ++u) s += sums[u * len + BIAS_FRONT + n];
-    s = wave_sum(s);
-    if (lane_id() == 0) out[a.max_distance] = s;
+  __device__ __forceinline__ void put(int dist, float v) {
+    if (dist >= max_distance) far += v;
+    else if (dist >= 0) out[dist] = v;
   }
-}
+  // The block at D0; returns nothing, keeps the sums of D0 - 63 .. D0.
+  __device__ __forceinline__ void block(int D0, const float (&acc)[NB][4]) {
+    const int l = lane_id(), g = l >> 4, c = l & 15;
+    float* to = rows + g * N + c;
+#pragma unroll
+    for (int i = -1; i < NB; ++i) {
+      float u = 0.f;
+      if (i >= 0) {   // lane c takes lane c + r (row_shl)
+        const int k = i < 0 ? 0 : i;
+        u = acc[k][0] + dpp_shift<0x101>(acc[k][1]) + dpp_shift<0x102>(acc[k][2]) + dpp_shift<0x103>(acc[k][3]);
+      }
+      if (i + 1 < NB) {   // lane c takes lane c + r - 16 of the next window (row_shr 16 - r)
+        const int k = i + 1 < NB ? i + 1 : 0;
+        u += dpp_shift<0x11F>(acc[k][1]) + dpp_shift<0x11E>(acc[k][2]) + dpp_shift<0x11D>(acc[k][3]);
+      }
+      to[16 * (i + 1)] = u;   // entry x of row g is distance D0 + x - 64 - 4 g
+    }
+    wave_lds_order();
+    float low = 0.f, high = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) low += rows[q * N + 1 + l + 4 * q];     // D0 - 63 + l
+    if (l < 16 * SUB - 1) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) high += rows[q * N + 65 + l + 4 * q]; // D0 + 1 + l
+    }
+    wave_lds_order();
+    put(D0 + 1 + l, carry + high);
+    carry = low;
+  }
+  // After the last block (at D0).
+  __device__ __forceinline__ void finish(int D0) {
+    put(D0 - 63 + lane_id(), carry);
+    far = wave_sum(far);
+    if (lane_id() == 0) out[max_distance] = far;
+  }
+};
 
 // ---------------------------------------------------------------------------------------
 template <typename T, int DH, bool DROP, bool BIAS>
@@ -199,7 +213,7 @@ __global__ void __launch_bounds__(NT) attn_fwd_kernel(QkvView<T> in, T* out, flo
     const int kv = s * 4 + (l >> 4);
     qf[s] = (qrow < S) ? ld16(Qp + (int64_t)qrow * in.ldq + kv * V) : u32x4{0, 0, 0, 0};
   }
-  if constexpr (BIAS) bias_build<NT>(bvec, bias, h, H);
+  if constexpr (BIAS) bias_build<NT, DH>(bvec, bias, h, H);
   floatx4 acc[DH / 16];
 #pragma unroll
   for (int t = 0; t < DH / 16; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -227,7 +241,7 @@ __global__ void __launch_bounds__(NT) attn_fwd_kernel(QkvView<T> in, T* out, flo
       for (int r = 0; r < 4; ++r) {
         const int key = k0 + kt * 16 + 4 * (l >> 4) + r;
         float x = st[kt][r] * scale_log2;
-        if constexpr (BIAS) x += bvec[BIAS_FRONT + min(max(qrow - key, 0), bias.max_distance)];
+        if constexpr (BIAS) x = (st[kt][r] + bvec[BIAS_FRONT + min(max(qrow - key, 0), bias.max_distance)]) * scale_log2;
         if (key > qrow || key >= S) x = -INFINITY;
         st[kt][r] = x;
         mx = fmaxf(mx, x);
@@ -412,9 +426,21 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
     blk_fill<CPR, C::NTF>(Kp + (int64_t)k0 * in.ldk, in.ldk, S - k0, st, wu, l);
     blk_fill<CPR, C::NTF>(Vp + (int64_t)k0 * in.ldv, in.ldv, S - k0, st + C::BLK * 16, wu, l);
   };
-  // raw scores q k^T of key block kb
-  auto scores = [&](int kb, floatx4 (&sc)[QS][4]) {
+  // with a bias, whether block kb has distances below far.from, which read the vector
+  FarValue far{0.f, 0};
+  auto is_near = [&](int kb) { return BIAS && qw0 - kb * BKV - (BKV - 1) < far.from; };
+  // raw scores q k^T of key block kb, with its bias where it reads the vector
+  auto scores = [&](auto vec, int kb, floatx4 (&sc)[QS][4]) {
     const u32x4* sK = ring + (kb % NS) * 2 * C::BLK;
+    const float* bp = decltype(vec)::value ? bvec + BIAS_FRONT + min(qw0 - kb * BKV, bias.max_distance + 63) + (l & 15) - 4 * g
+                                           : nullptr;
+    floatx4 b[QS + 3];   // of the tiles' distances qs - kt
+    if constexpr (decltype(vec)::value) {
+#pragma unroll
+      for (int i = 0; i < QS + 3; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) b[i][r] = bp[16 * (i - 3) - r];
+    }
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
       u32x4 kf[KS];
@@ -422,7 +448,8 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
       for (int s = 0; s < KS; ++s) kf[s] = blk_frag<CPR>(sK, s, kt * 16);
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) {
-        sc[qs][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (decltype(vec)::value) sc[qs][kt] = b[qs - kt + 3];
+        else sc[qs][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < KS; ++s) mma_step<bf16>(sc[qs][kt], kf[s], qf[qs][s]);
       }
@@ -430,20 +457,12 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   };
   // online softmax of block kb's scores: running max and sum, rescaled
   // accumulators, and the probabilities (dropped ones zeroed) as bf16 fragments
-  FarValue far{0.f, 0};
-  auto softmax = [&](auto masked, auto mode, int kb, floatx4 (&sc)[QS][4], u32x4 (&pf)[QS][2]) {
-    constexpr bool VEC = decltype(mode)::value == 2, FAR = decltype(mode)::value == 1;
+  auto softmax = [&](auto masked, auto is_far, int kb, floatx4 (&sc)[QS][4], u32x4 (&pf)[QS][2]) {
+    constexpr bool FAR = decltype(is_far)::value;
     const int k0 = kb * BKV;
-    const float* bp = VEC ? bvec + BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) + (l & 15) - 4 * g : nullptr;
 #pragma unroll
     for (int qs = 0; qs < QS; ++qs) {
       const int qrow = qw0 + 16 * qs + (l & 15);
-      if constexpr (VEC) {
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sc[qs][kt][r] = fmaf(sc[qs][kt][r], scale_log2, bp[16 * (qs - kt) - r]);
-      }
       if constexpr (decltype(masked)::value) {
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
@@ -459,15 +478,14 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
 #pragma unroll
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[qs][kt][r]);
       mx = group4_max(mx);
-      const float m_new = fmaxf(m_run[qs], VEC ? mx : FAR ? fmaf(mx, scale_log2, far.b) : mx * scale_log2);
+      const float m_new = fmaxf(m_run[qs], FAR ? fmaf(mx, scale_log2, far.b) : mx * scale_log2);
       const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
       const float alpha = fast_exp2(m_run[qs] - m_use);
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          sc[qs][kt][r] = fast_exp2(VEC ? sc[qs][kt][r] - m_use
-                                        : fmaf(sc[qs][kt][r], scale_log2, FAR ? far.b - m_use : -m_use));
+          sc[qs][kt][r] = fast_exp2(fmaf(sc[qs][kt][r], scale_log2, FAR ? far.b - m_use : -m_use));
       if constexpr (BIAS) {
         float rs = 0.f;
 #pragma unroll
@@ -535,12 +553,9 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
     if (kb + NS - 1 < nkb) fill(kb + NS - 1);
     if (kb > my_last) return;
     u32x4 pf[QS][2];
-    // with a bias, a block whose distances reach far.from takes the one value
-    using Near = std::conditional_t<BIAS, VecBias, NoBias>;
-    const bool near = !BIAS || qw0 - kb * BKV - (BKV - 1) < far.from;
-    auto inner = [&](auto mode) {
-      scores(kb + 1, nxt);
-      softmax(std::false_type{}, mode, kb, cur, pf);
+    auto inner = [&](auto vec_next, auto is_far) {   // the next block's scores beside this one's softmax
+      scores(vec_next, kb + 1, nxt);
+      softmax(std::false_type{}, is_far, kb, cur, pf);
       // interleave: the fragment reads first, then one MFMA per few ALU instructions
       __builtin_amdgcn_sched_group_barrier(0x100, 4 * KS, 0);
 #pragma unroll
@@ -549,17 +564,29 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
         __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
       }
     };
+    using Y = std::true_type;
+    using N = std::false_type;
     if constexpr (!PIPE) {
-      scores(kb, cur);
-      if (kb >= my_last) softmax(std::true_type{}, Near{}, kb, cur, pf);
-      else if (near) softmax(std::false_type{}, Near{}, kb, cur, pf);
-      else softmax(std::false_type{}, FarBias{}, kb, cur, pf);
+      const bool near = is_near(kb);
+      if constexpr (BIAS) {
+        if (near) scores(Y{}, kb, cur);
+        else scores(N{}, kb, cur);
+      } else {
+        scores(N{}, kb, cur);
+      }
+      if (kb >= my_last) softmax(Y{}, N{}, kb, cur, pf);
+      else if (!BIAS || near) softmax(N{}, N{}, kb, cur, pf);
+      else softmax(N{}, Y{}, kb, cur, pf);
     } else if (kb >= my_last) {
-      softmax(std::true_type{}, Near{}, kb, cur, pf);
-    } else if (near) {
-      inner(Near{});
-    } else if constexpr (BIAS) {
-      inner(FarBias{});
+      softmax(Y{}, N{}, kb, cur, pf);
+    } else if constexpr (!BIAS) {
+      inner(N{}, N{});
+    } else if (is_near(kb)) {   // key blocks come nearer: the next one is near too
+      inner(Y{}, N{});
+    } else if (is_near(kb + 1)) {
+      inner(Y{}, Y{});
+    } else {
+      inner(N{}, Y{});
     }
     pv(kb, pf);
   };
@@ -573,11 +600,18 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   // loop, which would also wait for the ring's prefetches
   wait_vmcnt_all();
   if constexpr (BIAS) {
-    bias_build<C::NTF>(bvec, bias, h, H);
-    far = bias_far(bvec, bias.max_distance);
+    bias_build<C::NTF, DH>(bvec, bias, h, H);
+    far = bias_far(bvec, bias.max_distance, scale_log2);
   }
   barrier_no_fence();
-  if (PIPE && my_last >= 0) scores(0, sA);
+  if (PIPE && my_last >= 0) {
+    if constexpr (BIAS) {
+      if (is_near(0)) scores(std::true_type{}, 0, sA);
+      else scores(std::false_type{}, 0, sA);
+    } else {
+      scores(std::false_type{}, 0, sA);
+    }
+  }
   for (int kb = 0; kb < nkb; kb += 2) {
     step(kb, sA, sB);
     if (kb + 1 < nkb) step(kb + 1, sB, sA);
@@ -664,7 +698,7 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(QkvView<T> in, const 
     kf[s] = (key < S) ? ld16(Kp + (int64_t)key * in.ldk + kv * V) : u32x4{0, 0, 0, 0};
     vf[s] = (key < S) ? ld16(Vp + (int64_t)key * in.ldv + kv * V) : u32x4{0, 0, 0, 0};
   }
-  if constexpr (BIAS) bias_build<NT>(bvec, bias, h, H);
+  if constexpr (BIAS) bias_build<NT, DH>(bvec, bias, h, H);
   floatx4 adk[DH / 16], adv[DH / 16];
 #pragma unroll
   for (int t = 0; t < DH / 16; ++t) adk[t] = adv[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -697,7 +731,7 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(QkvView<T> in, const 
         const int q = q0 + qi;
         const bool ok = (key <= q) && (q < S) && (key < S);
         const float bv = BIAS ? bvec[BIAS_FRONT + min(max(q - key, 0), bias.max_distance)] : 0.f;
-        const float p = ok ? exp2f((BIAS ? s[r] * scale_log2 + bv : s[r] * scale_log2) - sL[qi]) : 0.f;
+        const float p = ok ? exp2f((BIAS ? s[r] + bv : s[r]) * scale_log2 - sL[qi]) : 0.f;
         // dropout M = keep * scale: dV takes P M, dP = (dO V^T) M
         const float mk = DROP ? (((bits >> r) & 1) ? drop.scale : 0.f) : 1.f;
         P[qt][r] = p * mk;
@@ -764,12 +798,13 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(QkvView<T> in, const T*
     qf[s] = qok ? ld16(Qp + (int64_t)qrow * in.ldq + kv * V) : u32x4{0, 0, 0, 0};
     gf[s] = qok ? ld16(dOp + (int64_t)qrow * d + kv * V) : u32x4{0, 0, 0, 0};
   }
-  float* sums = nullptr;   // this wavefront's sums of dS by distance
+  DiagSums<1> diag;
   if constexpr (BIAS) {
-    sums = bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets;
-    for (int i = threadIdx.x; i < (NT / 64) * bias_len(bias.max_distance); i += NT) sums[i] = 0.f;
-    sums += w * bias_len(bias.max_distance);
-    bias_build<NT>(bvec, bias, h, H);
+    const int qw0 = q0 + 16 * w, nrow = (S + 15) / 16;
+    diag.init(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets,
+              bias.part != nullptr && qw0 < S ? bias.part + ((int64_t)bh * nrow + qw0 / 16) * (bias.max_distance + 1) : nullptr,
+              bias.max_distance);
+    bias_build<NT, DH>(bvec, bias, h, H);
   }
   floatx4 adq[DH / 16];
 #pragma unroll
@@ -798,19 +833,19 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(QkvView<T> in, const T*
         const int key = k0 + kt * 16 + 4 * (l >> 4) + r;
         const bool ok = qok && (key <= qrow) && (key < S);
         const float bv = BIAS ? bvec[BIAS_FRONT + min(max(qrow - key, 0), bias.max_distance)] : 0.f;
-        const float p = ok ? exp2f((BIAS ? s[r] * scale_log2 + bv : s[r] * scale_log2) - lq) : 0.f;
+        const float p = ok ? exp2f((BIAS ? s[r] + bv : s[r]) * scale_log2 - lq) : 0.f;
         const float mk = DROP ? (((bits >> r) & 1) ? drop.scale : 0.f) : 1.f;
         dS[kt][r] = p * (dp[r] * mk - Dq);
       }
     }
     if constexpr (BIAS) {
-      if (bias.part != nullptr) {   // uniform
+      if (diag.out != nullptr) {   // uniform in a wavefront
         float acc[4][4];
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) acc[3 - kt][r] = dS[kt][r];
-        bias_add_diagonals<4>(sums + BIAS_FRONT + min(q0 + 16 * w - k0, bias.max_distance + 63), acc);
+        diag.block(q0 + 16 * w - k0, acc);
       }
     }
 #pragma unroll
@@ -830,9 +865,7 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(QkvView<T> in, const T*
     }
   }
   if constexpr (BIAS) {
-    if (bias.part != nullptr)
-      bias_store_sums<NT / 64>(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets, bias, 0.f,
-                               bias.part + ((int64_t)bh * nqb + qb) * (bias.max_distance + 1));
+    if (diag.out != nullptr) diag.finish(q0 + 16 * w - last_kb * BKV);
   }
 }
 
@@ -990,8 +1023,8 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
   wait_vmcnt_all();   // kf and vf known complete: no vmcnt(0) inside the loop
   FarValue far{0.f, 0};
   if constexpr (BIAS) {
-    bias_build<C::NTB>(bvec, bias, h, H);
-    far = bias_far(bvec, bias.max_distance);
+    bias_build<C::NTB, DH>(bvec, bias, h, H);
+    far = bias_far(bvec, bias.max_distance, scale_log2);
   }
   for (int j = 0; j < njobs; ++j) {
     wait_loads<C::L, NS - 2>(min(njobs - 1, j + NS - 2) - j);
@@ -1007,9 +1040,21 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
     const bool edge = (q0 < kw0 + C::WR - 1) || (q0 + 64 > S) || (kw0 + C::WR > S);
     // the bias of query 16 t + 4 g + r and key 16 ks + l % 16 of these: bp[16 (t - ks) + r]
     const float* bp = BIAS ? bvec + BIAS_FRONT + min(q0 - kw0, bias.max_distance + C::WR - 1) + 4 * g - (l & 15) : nullptr;
+    const bool near = BIAS && (edge || q0 - kw0 - (C::WR - 1) < far.from);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {   // 32 queries: tiles 2s and 2s + 1
       floatx4 sc[SUB][2], dp[SUB][2];
+      floatx4 bv[SUB + 1];   // bias of the tiles' distances 2 s + u - ks (0 in a far block)
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int i = 0; i <= SUB; ++i) bv[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (near) {
+#pragma unroll
+          for (int i = 0; i <= SUB; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) bv[i][r] = bp[16 * (2 * s + i - SUB + 1) + r];
+        }
+      }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         u32x4 qfr[KST], gfr[KST];
@@ -1021,6 +1066,7 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
 #pragma unroll
         for (int ks = 0; ks < SUB; ++ks) {
           sc[ks][u] = dp[ks][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+          if constexpr (BIAS) sc[ks][u] = bv[u - ks + SUB - 1];
 #pragma unroll
           for (int st = 0; st < KST; ++st) {
             mma_step<bf16>(sc[ks][u], qfr[st], kf[ks][st]);
@@ -1032,18 +1078,16 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
       // Dropout M = keep * scale: dV takes P M, and dP = (dO V^T) M.
       uint32_t dbits[2][SUB];
       if constexpr (DROP) drop_col4_quad<SUB>(drop, bh, q0 + 32 * s, kw0, dbits);
-      auto softmax = [&](auto masked, auto mode) {
-        constexpr bool VEC = decltype(mode)::value == 2, FAR = decltype(mode)::value == 1;
+      auto softmax = [&](auto masked, auto is_far) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int qi = (2 * s + u) * 16 + 4 * g + r;
-            const float lq = FAR ? sP[2 * qi] - far.b : sP[2 * qi], Dq = sP[2 * qi + 1];
+            const float lq = decltype(is_far)::value ? sP[2 * qi] - far.b : sP[2 * qi], Dq = sP[2 * qi + 1];
 #pragma unroll
             for (int ks = 0; ks < SUB; ++ks) {
-              float x = VEC ? fmaf(sc[ks][u][r], scale_log2, bp[16 * (2 * s + u - ks) + r]) - lq
-                            : fmaf(sc[ks][u][r], scale_log2, -lq);
+              float x = fmaf(sc[ks][u][r], scale_log2, -lq);
               if constexpr (decltype(masked)::value) {
                 const int key = kw0 + 16 * ks + (l & 15);
                 x = (key <= q0 + qi && q0 + qi < S && key < S) ? x : -INFINITY;
@@ -1060,10 +1104,9 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
             }
           }
       };
-      using Near = std::conditional_t<BIAS, VecBias, NoBias>;
-      if (edge) softmax(std::true_type(), Near{});
-      else if (!BIAS || q0 - kw0 - (C::WR - 1) < far.from) softmax(std::false_type(), Near{});
-      else if constexpr (BIAS) softmax(std::false_type(), FarBias{});
+      if (edge) softmax(std::true_type(), std::false_type());
+      else if (!BIAS || near) softmax(std::false_type(), std::false_type());
+      else if constexpr (BIAS) softmax(std::false_type(), std::true_type());
       u32x4 pfr[SUB], dsf[SUB];
 #pragma unroll
       for (int ks = 0; ks < SUB; ++ks) {
@@ -1173,15 +1216,16 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
   for (int t = 0; t < NS - 1; ++t)
     if (t < nkb) fill(t);
   wait_vmcnt_all();   // qf, gf, lq and Dq known complete: no vmcnt(0) inside the loop
-  float* sums = nullptr;   // this wavefront's sums of dS by distance
-  float far_sum[4] = {0.f, 0.f, 0.f, 0.f};   // and over blocks beyond max_distance
+  DiagSums<SUB> sums;
+  float far_sum[4] = {0.f, 0.f, 0.f, 0.f};   // of dS over blocks beyond max_distance
   FarValue far{0.f, 0};
   if constexpr (BIAS) {
-    sums = bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets;
-    for (int i = threadIdx.x; i < C::WAVES * bias_len(bias.max_distance); i += C::NTB) sums[i] = 0.f;
-    sums += w * bias_len(bias.max_distance);
-    bias_build<C::NTB>(bvec, bias, h, H);
-    far = bias_far(bvec, bias.max_distance);
+    const int nrow = (S + C::WR - 1) / C::WR;
+    sums.init(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets,
+              bias.part != nullptr && qw0 < S ? bias.part + ((int64_t)bh * nrow + qw0 / C::WR) * (bias.max_distance + 1) : nullptr,
+              bias.max_distance);
+    bias_build<C::NTB, DH>(bvec, bias, h, H);
+    far = bias_far(bvec, bias.max_distance, scale_log2);
   }
   for (int kb = 0; kb < nkb; ++kb) {
     wait_loads<C::L, NS - 2>(min(nkb - 1, kb + NS - 2) - kb);
@@ -1194,8 +1238,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
     const int k0 = kb * BKV;
     const bool edge = (k0 + BKV - 1 > qw0) || (k0 + BKV > S) || (qw0 + C::WR > S);
     const bool near = !BIAS || edge || qw0 - k0 - (BKV - 1) < far.from;
-    const int dist = BIAS ? BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) : 0;   // entry of the block's own distance
-    const float* bp = BIAS ? bvec + dist + (l & 15) - 4 * g : nullptr;
+    const float* bp = BIAS ? bvec + BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) + (l & 15) - 4 * g : nullptr;
     float diag[SUB + 3][4];
     if constexpr (BIAS) {
 #pragma unroll
@@ -1206,6 +1249,17 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
 #pragma unroll
     for (int s = 0; s < 2; ++s) {   // 32 keys: tiles 2s and 2s + 1
       floatx4 sc[SUB][2], dp[SUB][2];
+      floatx4 bv[SUB + 1];   // bias of the tiles' distances qs - 2 s - u (0 in a far block)
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int i = 0; i <= SUB; ++i) bv[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (near) {
+#pragma unroll
+          for (int i = 0; i <= SUB; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) bv[i][r] = bp[16 * (i - 1 - 2 * s) - r];
+        }
+      }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         u32x4 kfr[KST], vfr[KST];
@@ -1217,6 +1271,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
 #pragma unroll
         for (int qs = 0; qs < SUB; ++qs) {
           sc[qs][u] = dp[qs][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+          if constexpr (BIAS) sc[qs][u] = bv[qs - u + 1];
 #pragma unroll
           for (int st = 0; st < KST; ++st) {
             mma_step<bf16>(sc[qs][u], kfr[st], qf[qs][st]);
@@ -1224,8 +1279,8 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
           }
         }
       }
-      auto softmax = [&](auto masked, auto mode) {
-        constexpr bool VEC = decltype(mode)::value == 2, FAR = decltype(mode)::value == 1;
+      auto softmax = [&](auto masked, auto is_far) {
+        constexpr bool FAR = decltype(is_far)::value;
 #pragma unroll
         for (int qs = 0; qs < SUB; ++qs) {
           const float lqb = FAR ? lq[qs] - far.b : lq[qs];
@@ -1237,8 +1292,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
             const uint32_t bits = dbits[u];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float x = VEC ? fmaf(sc[qs][u][r], scale_log2, bp[16 * (qs - 2 * s - u) - r]) - lqb
-                            : fmaf(sc[qs][u][r], scale_log2, -lqb);
+              float x = fmaf(sc[qs][u][r], scale_log2, -lqb);
               if constexpr (decltype(masked)::value) {
                 const int key = k0 + (2 * s + u) * 16 + 4 * g + r;
                 x = (key <= q && key < S && q < S) ? x : -INFINITY;
@@ -1246,16 +1300,15 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
               const float p = fast_exp2(x);
               const float mk = DROP ? (((bits >> r) & 1) ? drop.scale : 0.f) : 1.f;
               dp[qs][u][r] = p * (dp[qs][u][r] * mk - Dq[qs]);
-              if constexpr (VEC) diag[qs - 2 * s - u + 3][r] += dp[qs][u][r];
+              if constexpr (BIAS && !FAR) diag[qs - 2 * s - u + 3][r] += dp[qs][u][r];
               if constexpr (FAR) far_sum[r] += dp[qs][u][r];
             }
           }
         }
       };
-      using Near = std::conditional_t<BIAS, VecBias, NoBias>;
-      if (edge) softmax(std::true_type(), Near{});
-      else if (near) softmax(std::false_type(), Near{});
-      else if constexpr (BIAS) softmax(std::false_type(), FarBias{});
+      if (edge) softmax(std::true_type(), std::false_type());
+      else if (near) softmax(std::false_type(), std::false_type());
+      else if constexpr (BIAS) softmax(std::false_type(), std::true_type());
       u32x4 dsf[SUB];
 #pragma unroll
       for (int qs = 0; qs < SUB; ++qs) dsf[qs] = acc_to_frag<bf16>(dp[qs], 0);
@@ -1267,7 +1320,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
       }
     }
     if constexpr (BIAS) {
-      if (near && bias.part != nullptr) bias_add_diagonals<SUB + 3>(sums + dist, diag);
+      if (near && sums.out != nullptr) sums.block(qw0 - k0, diag);
     }
   }
 #pragma unroll
@@ -1283,10 +1336,10 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
     }
   }
   if constexpr (BIAS) {
-    if (bias.part != nullptr)
-      bias_store_sums<C::WAVES>(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets, bias,
-                                (far_sum[0] + far_sum[1]) + (far_sum[2] + far_sum[3]),
-                                bias.part + ((int64_t)bh * nqb + qb) * (bias.max_distance + 1));
+    if (sums.out != nullptr) {
+      sums.far += (far_sum[0] + far_sum[1]) + (far_sum[2] + far_sum[3]);
+      sums.finish(qw0 - my_last * BKV);
+    }
   }
   if (grad.sq != nullptr) {   // uniform: bias gradient += column sums of dQ over this workgroup's queries
     float v[DH / 16][4];
@@ -1325,40 +1378,44 @@ __global__ void __launch_bounds__((BwdRing<DH, SMALL>::NTB), (BwdRing<DH, SMALL>
                                         drop, bias);
 }
 
-// g_table[bucket][h] += sum over the rows (sequences and query blocks) of head h of
-// part [rows][n = max_distance + 1], by bucket. One workgroup per head: the rows are
-// summed per distance (a fixed number of row groups, each in order), then a wavefront
-// sums the distances of a bucket.
+// g_table[b][h] += the sum over sequences, wavefronts (wr queries each, `rows` of them) and
+// the distances of bucket b of part [sequence][head][wavefront][max_distance + 1]. A
+// wavefront has entries for the distances its queries reach. One workgroup per bucket and
+// head, a fixed order.
 constexpr int BS_NT = 1024;
-__global__ void __launch_bounds__(BS_NT) attn_bias_sums_kernel(const float* __restrict__ part, int batch, int blocks, int H,
+__global__ void __launch_bounds__(BS_NT) attn_bias_sums_kernel(const float* __restrict__ part, int batch, int rows, int wr, int H,
                                                                const int32_t* __restrict__ bounds, int n_buckets,
                                                                int max_distance, float* g_table) {
-  __shared__ float red[BS_NT];
-  __shared__ float dist[MAX_DISTANCE + 1];
-  const int h = blockIdx.x, n = max_distance + 1, rows = batch * blocks;
-  const int cl = threadIdx.x & 63, rg = threadIdx.x >> 6;   // 64 distances x 16 row groups
-  for (int n0 = 0; n0 < n; n0 += 64) {
-    float s = 0.f;
-    if (n0 + cl < n) {
-#pragma unroll 4
-      for (int r = rg; r < rows; r += BS_NT / 64)
-        s += part[(((int64_t)(r / blocks) * H + h) * blocks + r % blocks) * n + n0 + cl];
+  __shared__ float red[BS_NT / 64];
+  const int b = blockIdx.x, h = blockIdx.y, n = max_distance + 1;
+  const int lo = b == 0 ? 0 : min(max(bounds[b], 0), n), hi = b + 1 < n_buckets ? min(max(bounds[b + 1], 0), n) : n;
+  const int width = hi - lo;
+  float s = 0.f;
+  if (width > 0) {   // uniform
+    int cw = 1;   // threads along a row
+    while (cw < width && cw < 64) cw *= 2;
+    const int c = threadIdx.x & (cw - 1), step = BS_NT / cw, total = batch * rows;
+    for (int d = lo + c; d < hi; d += cw) {
+      for (int row0 = threadIdx.x / cw; row0 < total; row0 += 8 * step) {
+        float v[8];   // loads first; entries beyond a wavefront's reach hold anything
+        bool ok[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int row = min(row0 + k * step, total - 1), seq = row / rows, w = row - seq * rows;
+          ok[k] = row0 + k * step < total && (d == max_distance || d < (w + 1) * wr);
+          v[k] = part[(((int64_t)seq * H + h) * rows + w) * n + d];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += ok[k] ? v[k] : 0.f;
+      }
     }
-    red[threadIdx.x] = s;
-    __syncthreads();
-    if (rg == 0 && n0 + cl < n) {
-      for (int q = 1; q < BS_NT / 64; ++q) s += red[q * 64 + cl];
-      dist[n0 + cl] = s;
-    }
-    __syncthreads();
   }
-  for (int b = rg; b < n_buckets; b += BS_NT / 64) {
-    const int lo = b == 0 ? 0 : max(bounds[b], 0), hi = b + 1 < n_buckets ? min(bounds[b + 1], n) : n;
-    float s = 0.f;
-    for (int i = lo + cl; i < hi; i += 64) s += dist[i];
-    s = wave_sum(s);
-    if (cl == 0) g_table[(int64_t)b * H + h] += s;
-  }
+  s = wave_sum(s);
+  if (lane_id() == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < BS_NT / 64; ++w) s += red[w];
+  g_table[(int64_t)b * H + h] += s;
 }
 
 // Whether workgroups of 64 rows (SMALL) fit the CUs about twice, so that the
@@ -1372,9 +1429,9 @@ template <typename T> QkvView<T> view(const AttnArgs& a) {
           a.ldv};
 }
 BiasArgs bias_args(const AttnArgs& a) { return {a.table, a.bounds, a.n_buckets, a.max_distance, nullptr}; }
-// bytes of LDS behind the tiles
-size_t bias_lds(const AttnArgs& a, int waves) {
-  return a.table ? sizeof(float) * (size_t)bias_lds_floats(a.max_distance, a.n_buckets, waves) : 0;
+// bytes of LDS behind the tiles; diag: floats of the wavefronts' DiagRows
+size_t bias_lds(const AttnArgs& a, int diag) {
+  return a.table ? sizeof(float) * (size_t)bias_lds_floats(a.max_distance, a.n_buckets, diag) : 0;
 }
 
 template <typename T, int DH>
@@ -1405,15 +1462,10 @@ hipError_t fwd_launch(const AttnArgs& a, void* o, float* lse2, hipStream_t st) {
   return a.table ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
-// Query blocks of the dQ workgroups: 64 queries, or as many as the ring's larger ones take.
-template <int DH> int dq_rows(int64_t heads, int S) {
-  return small_grid(2 * heads, S) ? BwdRing<DH, true>::BR : BwdRing<DH, false>::BR;
-}
-int dq_blocks(const AttnArgs& a) {
-  const int64_t heads = (int64_t)a.mu * a.H;
-  int rows = 64;
-  if (a.dt == DT_BF16) rows = a.dh == 32 ? dq_rows<32>(heads, a.S) : a.dh == 64 ? dq_rows<64>(heads, a.S) : dq_rows<128>(heads, a.S);
-  return (a.S + rows - 1) / rows;
+// Queries of a dQ wavefront.
+int dq_wave_rows(const AttnArgs& a) {
+  if (a.dt != DT_BF16 || small_grid(2 * (int64_t)a.mu * a.H, a.S)) return 16;
+  return a.dh == 32 ? BwdRing<32>::WR : a.dh == 64 ? BwdRing<64>::WR : BwdRing<128>::WR;
 }
 
 template <typename T, int DH>
@@ -1445,7 +1497,7 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
         const int ny = (S + C::BR - 1) / C::BR;
         const dim3 grid(mu * H, 2 * ny);   // dK/dV blocks, then dQ blocks
         auto k = a.drop.thr ? attn_bwd_ring_kernel<DH, true, SM, B> : attn_bwd_ring_kernel<DH, false, SM, B>;
-        hipLaunchKernelGGL(k, grid, dim3(C::NTB), bias_lds(a, C::WAVES), st, view<T>(a), g, ws, grad, S, S_pad, H, d,
+        hipLaunchKernelGGL(k, grid, dim3(C::NTB), bias_lds(a, C::WAVES * DiagRow<C::SUB>::FLOATS), st, view<T>(a), g, ws, grad, S, S_pad, H, d,
                            scale_log2, scale, a.drop, ny, ba);
       };
       if (small_grid(2 * (int64_t)mu * H, S)) go(std::true_type{});
@@ -1463,7 +1515,7 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
       e = hipGetLastError();
       if (e != hipSuccess) return e;
       auto dqk = a.drop.thr ? attn_bwd_dq_kernel<T, DH, true, B> : attn_bwd_dq_kernel<T, DH, false, B>;
-      hipLaunchKernelGGL(dqk, dim3((S + 63) / 64, mu * H), dim3(NT), bias_lds(a, NT / 64), st, view<T>(a), g, lse2, ws, grad, S,
+      hipLaunchKernelGGL(dqk, dim3((S + 63) / 64, mu * H), dim3(NT), bias_lds(a, NT / 64 * DiagRow<1>::FLOATS), st, view<T>(a), g, lse2, ws, grad, S,
                          H, d, scale_log2, scale, a.drop, ba);
       e = hipGetLastError();
       // column sums: one pass where all three lie side by side
@@ -1478,8 +1530,9 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
   };
   hipError_t e = a.table ? launch(std::true_type{}) : launch(std::false_type{});
   if (e != hipSuccess || ba.part == nullptr) return e;
-  hipLaunchKernelGGL(attn_bias_sums_kernel, dim3(H), dim3(BS_NT), 0, st, ba.part, mu, dq_blocks(a), H, a.bounds, a.n_buckets,
-                     a.max_distance, gr.g_table);
+  const int wr = dq_wave_rows(a);
+  hipLaunchKernelGGL(attn_bias_sums_kernel, dim3(a.n_buckets, H), dim3(BS_NT), 0, st, ba.part, mu, (S + wr - 1) / wr, wr, H,
+                     a.bounds, a.n_buckets, a.max_distance, gr.g_table);
   return hipGetLastError();
 }
 
@@ -1510,7 +1563,8 @@ int64_t attn_bwd_workspace_floats(DType dt, int mu, int S, int H) {
   return (int64_t)mu * H * S;
 }
 int64_t attn_bias_workspace_floats(const AttnArgs& a) {
-  return (int64_t)a.mu * a.H * dq_blocks(a) * (a.max_distance + 1);
+  const int wr = dq_wave_rows(a);
+  return (int64_t)a.mu * a.H * ((a.S + wr - 1) / wr) * (a.max_distance + 1);
 }
 
 hipError_t attn_bwd(const AttnArgs& a, const AttnGrads& g, const void* o, const void* dO, const float* lse2, float* ws,

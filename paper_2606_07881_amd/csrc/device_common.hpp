@@ -290,9 +290,11 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_shift(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
 }
-// Adds v to a float in LDS (one instruction, no result).
-__device__ __forceinline__ void lds_add(float* p, float v) {
-  (void)__hip_atomic_fetch_add((__attribute__((address_space(3))) float*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+// Between LDS stores of a wavefront and LDS loads of the same words by its other lanes: the LDS
+// serves a wavefront's accesses in order, so only the compiler has to keep theirs.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
 }
 __device__ __forceinline__ float row_sum16(float v) {
   v += dpp_f<0xB1>(v);    // quad_perm [1, 0, 3, 2]
