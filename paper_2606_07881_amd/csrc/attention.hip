@@ -59,7 +59,8 @@ struct BiasArgs {
   const float* table;      // [n_buckets][H]
   const int32_t* bounds;   // first distance of every bucket, ascending
   int n_buckets, max_distance;
-  float* part;             // dQ wavefronts: sums of dS by distance, [heads][wavefront][max_distance + 1], or null
+  int batch;
+  float* part;             // dQ wavefronts: sums of dS by distance, [H][batch][wavefront][max_distance + 1], or null
 };
 constexpr int BIAS_FRONT = 80, BIAS_TAIL = 128;   // distances below 0 (masked keys) and above max_distance inside a window
 constexpr float BIAS_MASKED = -1e30f;
@@ -802,7 +803,7 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(QkvView<T> in, const T*
   if constexpr (BIAS) {
     const int qw0 = q0 + 16 * w, nrow = (S + 15) / 16;
     diag.init(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets,
-              bias.part != nullptr && qw0 < S ? bias.part + ((int64_t)bh * nrow + qw0 / 16) * (bias.max_distance + 1) : nullptr,
+              bias.part != nullptr && qw0 < S ? bias.part + (((int64_t)h * bias.batch + b) * nrow + qw0 / 16) * (bias.max_distance + 1) : nullptr,
               bias.max_distance);
     bias_build<NT, DH>(bvec, bias, h, H);
   }
@@ -1222,7 +1223,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
   if constexpr (BIAS) {
     const int nrow = (S + C::WR - 1) / C::WR;
     sums.init(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets,
-              bias.part != nullptr && qw0 < S ? bias.part + ((int64_t)bh * nrow + qw0 / C::WR) * (bias.max_distance + 1) : nullptr,
+              bias.part != nullptr && qw0 < S ? bias.part + (((int64_t)h * bias.batch + b) * nrow + qw0 / C::WR) * (bias.max_distance + 1) : nullptr,
               bias.max_distance);
     bias_build<C::NTB, DH>(bvec, bias, h, H);
     far = bias_far(bvec, bias.max_distance, scale_log2);
@@ -1379,43 +1380,66 @@ __global__ void __launch_bounds__((BwdRing<DH, SMALL>::NTB), (BwdRing<DH, SMALL>
 }
 
 // g_table[b][h] += the sum over sequences, wavefronts (wr queries each, `rows` of them) and
-// the distances of bucket b of part [sequence][head][wavefront][max_distance + 1]. A
-// wavefront has entries for the distances its queries reach. One workgroup per bucket and
-// head, a fixed order.
-constexpr int BS_NT = 1024;
+// the distances of bucket b of part [head][sequence][wavefront][max_distance + 1]. A
+// wavefront has entries for the distances its queries reach. A workgroup takes the buckets
+// of a head that begin at one of 32 distances (32 blockIdx.x and on): it sums their
+// distances over the rows, side by side, then a wavefront adds up a bucket. All in a fixed
+// order. (A workgroup per bucket reads narrow columns, which every XCD fetches again: 17 us
+// for 4 x 128 rows of 257 and 16 heads.)
+constexpr int BS_NT = 512, BS_SPAN = 32;
 __global__ void __launch_bounds__(BS_NT) attn_bias_sums_kernel(const float* __restrict__ part, int batch, int rows, int wr, int H,
                                                                const int32_t* __restrict__ bounds, int n_buckets,
                                                                int max_distance, float* g_table) {
-  __shared__ float red[BS_NT / 64];
-  const int b = blockIdx.x, h = blockIdx.y, n = max_distance + 1;
-  const int lo = b == 0 ? 0 : min(max(bounds[b], 0), n), hi = b + 1 < n_buckets ? min(max(bounds[b + 1], 0), n) : n;
-  const int width = hi - lo;
-  float s = 0.f;
-  if (width > 0) {   // uniform
-    int cw = 1;   // threads along a row
-    while (cw < width && cw < 64) cw *= 2;
-    const int c = threadIdx.x & (cw - 1), step = BS_NT / cw, total = batch * rows;
-    for (int d = lo + c; d < hi; d += cw) {
-      for (int row0 = threadIdx.x / cw; row0 < total; row0 += 8 * step) {
-        float v[8];   // loads first; entries beyond a wavefront's reach hold anything
-        bool ok[8];
+  __shared__ float red[BS_NT];
+  __shared__ float dist[MAX_DISTANCE + 1];
+  __shared__ int begin[MAX_BUCKETS + 1];   // first distance of every bucket, and the end
+  const int h = blockIdx.y, n = max_distance + 1, c = threadIdx.x & 63, rg = threadIdx.x >> 6;
+  for (int b = threadIdx.x; b <= n_buckets; b += BS_NT)
+    begin[b] = b == 0 ? 0 : b < n_buckets ? min(max(bounds[b], 0), n) : n;
+  __syncthreads();
+  int b0 = 0, b1 = 0;   // the workgroup's buckets
+  for (int b = c; b < n_buckets; b += 64) {   // every wavefront counts for itself
+    b0 += begin[b] < BS_SPAN * (int)blockIdx.x;
+    b1 += begin[b] < BS_SPAN * ((int)blockIdx.x + 1);
+  }
+  b0 = (int)wave_sum((float)b0);
+  b1 = (int)wave_sum((float)b1);
+  if (b0 >= b1) return;   // uniform
+  const int first = begin[b0], last = begin[b1], total = batch * rows;
+  int cw = BS_SPAN;   // distances side by side: all of them if they are at most 128
+  while (cw < last - first && cw < 128) cw *= 2;
+  const int cc = threadIdx.x & (cw - 1), r0 = threadIdx.x / cw, step = BS_NT / cw;
+  const float* mine = part + (int64_t)h * total * n;
+  const int turn = step % rows;   // how far a step moves within the wavefronts of a sequence
+  for (int d0 = first; d0 < last; d0 += cw) {
+    const int d = min(d0 + cc, max_distance);
+    float s = 0.f;
+    int w = r0 % rows;
+    for (int row0 = r0; row0 < total; row0 += 16 * step) {
+      float v[16];   // loads first; entries beyond a wavefront's reach hold anything
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int row = min(row0 + k * step, total - 1), seq = row / rows, w = row - seq * rows;
-          ok[k] = row0 + k * step < total && (d == max_distance || d < (w + 1) * wr);
-          v[k] = part[(((int64_t)seq * H + h) * rows + w) * n + d];
-        }
+      for (int k = 0; k < 16; ++k) v[k] = mine[(int64_t)min(row0 + k * step, total - 1) * n + d];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s += ok[k] ? v[k] : 0.f;
+      for (int k = 0; k < 16; ++k) {
+        s += row0 + k * step < total && (d == max_distance || d < (w + 1) * wr) ? v[k] : 0.f;
+        w += turn;
+        if (w >= rows) w -= rows;
       }
     }
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (r0 == 0 && d0 + cc < n) {
+      for (int q = 1; q < step; ++q) s += red[q * cw + cc];
+      dist[d0 + cc] = s;
+    }
+    __syncthreads();
   }
-  s = wave_sum(s);
-  if (lane_id() == 0) red[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  for (int w = 1; w < BS_NT / 64; ++w) s += red[w];
-  g_table[(int64_t)b * H + h] += s;
+  for (int b = b0 + rg; b < b1; b += BS_NT / 64) {
+    float s = 0.f;
+    for (int i = begin[b] + c; i < begin[b + 1]; i += 64) s += dist[i];
+    s = wave_sum(s);
+    if (c == 0) g_table[(int64_t)b * H + h] += s;
+  }
 }
 
 // Whether workgroups of 64 rows (SMALL) fit the CUs about twice, so that the
@@ -1428,7 +1452,7 @@ template <typename T> QkvView<T> view(const AttnArgs& a) {
   return {reinterpret_cast<const T*>(a.q), reinterpret_cast<const T*>(a.k), reinterpret_cast<const T*>(a.v), a.ldq, a.ldk,
           a.ldv};
 }
-BiasArgs bias_args(const AttnArgs& a) { return {a.table, a.bounds, a.n_buckets, a.max_distance, nullptr}; }
+BiasArgs bias_args(const AttnArgs& a) { return {a.table, a.bounds, a.n_buckets, a.max_distance, a.mu, nullptr}; }
 // bytes of LDS behind the tiles; diag: floats of the wavefronts' DiagRows
 size_t bias_lds(const AttnArgs& a, int diag) {
   return a.table ? sizeof(float) * (size_t)bias_lds_floats(a.max_distance, a.n_buckets, diag) : 0;
@@ -1531,7 +1555,7 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
   hipError_t e = a.table ? launch(std::true_type{}) : launch(std::false_type{});
   if (e != hipSuccess || ba.part == nullptr) return e;
   const int wr = dq_wave_rows(a);
-  hipLaunchKernelGGL(attn_bias_sums_kernel, dim3(a.n_buckets, H), dim3(BS_NT), 0, st, ba.part, mu, (S + wr - 1) / wr, wr, H,
+  hipLaunchKernelGGL(attn_bias_sums_kernel, dim3(a.max_distance / BS_SPAN + 1, H), dim3(BS_NT), 0, st, ba.part, mu, (S + wr - 1) / wr, wr, H,
                      a.bounds, a.n_buckets, a.max_distance, gr.g_table);
   return hipGetLastError();
 }
