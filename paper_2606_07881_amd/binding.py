@@ -424,8 +424,10 @@ class Stage:
 # ---- attention operators (device) ------------------------------------------------------------
 # Each runs on the tensors' device and its current torch stream. Matrices are
 # [rows, columns] with contiguous rows (any row stride the C ABI admits, e.g. a
-# column range of a fused projection); vectors are contiguous.
+# column range of a fused projection); vectors are contiguous. The checks are
+# written for few Python operations: a small call costs more here than on the GPU.
 _TORCH_DTYPES = {torch.bfloat16: BF16, torch.float32: FP32}
+_F32, _I32, _F64 = torch.float32, torch.int32, torch.float64
 
 
 def rope_freqs(theta, rope_dims):
@@ -444,38 +446,38 @@ def rel_bounds(n_buckets, max_distance):
     return b
 
 
-def _mat(t, rows, cols, like, where):
-    """Pointer and row stride of a [rows, cols] tensor of like's dtype and device."""
-    if (t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != like.dtype or t.device != like.device
-            or (cols > 1 and t.numel() and t.stride(1) != 1)):
-        raise PaciError(E_INVAL, f"{where}: [{rows}, {cols}] {like.dtype} on {like.device} with contiguous rows expected")
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0)
+def _refuse(what, code=E_INVAL):
+    raise PaciError(code, what)
 
 
-def _vec(t, shape, dtype, like, where):
-    """Pointer of a contiguous tensor of this shape (None: null)."""
+def _mat(t, shape, like, what):
+    """Address of a matrix of this shape and of like's dtype and device (its stride is the caller's to pass)."""
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device or (t.stride(1) != 1 and shape[1] > 1):
+        _refuse(f"{what}: {tuple(shape)} {like.dtype} on {like.device} with contiguous rows expected")
+    return t.data_ptr()
+
+
+def _vec(t, shape, dtype, like, what):
+    """Address of a contiguous tensor of this shape (None: null)."""
     if t is None:
         return None
-    if tuple(t.shape) != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous():
-        raise PaciError(E_INVAL, f"{where}: contiguous {shape} {dtype} on {like.device} expected")
-    return ctypes.c_void_p(t.data_ptr())
+    if t.shape != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous():
+        _refuse(f"{what}: contiguous {shape} {dtype} on {like.device} expected")
+    return t.data_ptr()
 
 
-def _operand(x, where):
-    """Checks what every operator asks of its first tensor; returns the PACI dtype."""
-    if x.device.type != "cuda":
-        raise PaciError(E_INVAL, f"{where}: a device tensor expected")
-    if x.dim() != 2:
-        raise PaciError(E_INVAL, f"{where}: a matrix expected")
-    if x.dtype not in _TORCH_DTYPES:
-        raise PaciError(E_UNSUPPORTED, where)
-    return _TORCH_DTYPES[x.dtype]
+def _operand(x, what):
+    """The PACI dtype of an operator's first tensor, a matrix on a device."""
+    if not x.is_cuda or x.dim() != 2:
+        _refuse(f"{what}: a device matrix expected")
+    dt = _TORCH_DTYPES.get(x.dtype)
+    return _refuse(what, E_UNSUPPORTED) if dt is None else dt
 
 
 def _launch(fn, like, *args):
     """Calls a C operator on like's device and current stream."""
-    dev = like.device.index
-    st = ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+    dev = like.get_device()
+    st = torch.cuda.current_stream(dev).cuda_stream
     if dev == torch.cuda.current_device():
         r = fn(*args, st)
     else:
@@ -485,53 +487,31 @@ def _launch(fn, like, *args):
         raise PaciError(r, fn.__name__, lib.paci_last_hip_error(None) if r == E_HIP else 0)
 
 
-def _workspace(ws, fn, shapes, like):
-    """The caller's workspace (any contiguous tensor on the device), or one of the needed
-    size from torch's allocator on the current stream: (tensor, bytes)."""
-    if ws is None:
-        n = ctypes.c_size_t(0)
-        _check(fn(ctypes.byref(shapes), ctypes.byref(n)), fn.__name__)
-        return torch.empty(n.value, dtype=torch.uint8, device=like.device), n.value
-    if ws.device != like.device or not ws.is_contiguous():
-        raise PaciError(E_INVAL, f"{fn.__name__}: a contiguous workspace on {like.device} expected")
-    return ws, ws.numel() * ws.element_size()
-
-
-def qk_norm_rope_workspace(*args, **kw):
-    """Bytes of workspace qk_norm_rope_backward needs (its x, dx and shape arguments; ws excluded)."""
-    return _bytes(lib.paci_qk_norm_rope_workspace, _qk_shapes(*args, **kw))
-
-
-def attention_workspace(*args, **kw):
-    """Bytes of workspace attention_backward needs (q and the arguments of _attn_shapes)."""
-    return _bytes(lib.paci_attn_workspace, _attn_shapes(*args, **kw))
-
-
 def _bytes(fn, shapes):
     n = ctypes.c_size_t(0)
     _check(fn(ctypes.byref(shapes), ctypes.byref(n)), fn.__name__)
     return n.value
 
 
+def _workspace(ws, fn, shapes, like):
+    """The caller's workspace (any contiguous tensor on the device), or one of the needed
+    size from torch's allocator on the current stream: (tensor, bytes)."""
+    if ws is None:
+        n = _bytes(fn, shapes)
+        return like.new_empty((n + 3) // 4, dtype=_F32), n
+    if ws.device != like.device or not ws.is_contiguous():
+        _refuse(f"{fn.__name__}: a contiguous workspace on {like.device} expected")
+    return ws, ws.numel() * ws.element_size()
+
+
 def _qk_shapes(x, q_heads, k_heads, seq, norm, eps, freq, pairs):
-    where = "qk_norm_rope"
-    s = PaciQkShapes(dtype=_operand(x, where), tokens=x.shape[0], seq=seq, q_heads=q_heads, k_heads=k_heads, norm=int(norm),
-                     eps=eps, rope_dims=0 if freq is None else 2 * freq.numel())
+    dt = _operand(x, "qk_norm_rope x")
+    tokens, cols = x.shape
     heads = q_heads + k_heads
-    if heads < 1 or x.shape[1] % heads:
-        raise PaciError(E_INVAL, f"{where}: {x.shape[1]} columns do not hold {heads} heads")
-    if pairs not in ROPE_PAIRS:
-        raise PaciError(E_INVAL, f"{where}: pairs {pairs!r}")
-    s.head_dim = x.shape[1] // heads
-    s.rope_pairs = ROPE_PAIRS[pairs]
-    return s
-
-
-def _qk_params(s, x, q_gain, k_gain, pos, freq, where):
-    dh = (s.head_dim,)
-    return [_vec(q_gain, dh, torch.float32, x, where + " q_gain"), _vec(k_gain, dh, torch.float32, x, where + " k_gain"),
-            _vec(pos, (s.tokens,), torch.int32, x, where + " pos"),
-            _vec(freq, (s.rope_dims // 2,), torch.float64, x, where + " freq")]
+    if heads < 1 or cols % heads or pairs not in ROPE_PAIRS:
+        _refuse(f"qk_norm_rope: {cols} columns of {heads} heads, pairs {pairs!r}")
+    return PaciQkShapes(dt, tokens, seq, q_heads, k_heads, cols // heads, norm, eps, 0 if freq is None else 2 * freq.numel(),
+                        ROPE_PAIRS[pairs])
 
 
 def qk_norm_rope(x, y, q_heads, k_heads, seq=1, q_gain=None, k_gain=None, eps=1e-5, freq=None, pairs="half", pos=None):
@@ -539,13 +519,18 @@ def qk_norm_rope(x, y, q_heads, k_heads, seq=1, q_gain=None, k_gain=None, eps=1e
     [tokens, (q_heads + k_heads) * head_dim]. Gains ([head_dim] float32): norm, None:
     no norm. freq ([rope_dims / 2] float64): rotation, None: none. pos ([tokens] int32)
     or, without it, row % seq. y may be x."""
-    where = "qk_norm_rope"
     s = _qk_shapes(x, q_heads, k_heads, seq, q_gain is not None or k_gain is not None, eps, freq, pairs)
-    xp, ldx = _mat(x, *x.shape, x, where + " x")
-    yp, ldy = _mat(y, *x.shape, x, where + " y")
-    gq, gk, pp, fp = _qk_params(s, x, q_gain, k_gain, pos, freq, where)
-    _launch(lib.paci_qk_norm_rope_forward, x, ctypes.byref(s), xp, ldx, gq, gk, pp, fp, yp, ldy)
+    dh = (s.head_dim,)
+    _launch(lib.paci_qk_norm_rope_forward, x, ctypes.byref(s), _mat(x, x.shape, x, "qk_norm_rope x"), x.stride(0),
+            _vec(q_gain, dh, _F32, x, "q_gain"), _vec(k_gain, dh, _F32, x, "k_gain"),
+            _vec(pos, (s.tokens,), _I32, x, "pos"), _vec(freq, (s.rope_dims // 2,), _F64, x, "freq"),
+            _mat(y, x.shape, x, "qk_norm_rope y"), y.stride(0))
     return y
+
+
+def qk_norm_rope_workspace(x, q_heads, k_heads, seq=1, norm=True, freq=None, pairs="half"):
+    """Bytes of workspace that qk_norm_rope_backward needs for these operands."""
+    return _bytes(lib.paci_qk_norm_rope_workspace, _qk_shapes(x, q_heads, k_heads, seq, norm, 0.0, freq, pairs))
 
 
 def qk_norm_rope_backward(x, dy, dx, q_heads, k_heads, seq=1, q_gain=None, k_gain=None, eps=1e-5, freq=None, pairs="half",
@@ -553,78 +538,63 @@ def qk_norm_rope_backward(x, dy, dx, q_heads, k_heads, seq=1, q_gain=None, k_gai
     """paci_qk_norm_rope_backward: dx from dy and the forward's arguments; g_q_gain, g_k_gain
     and g_bias (float32, optional) are added to. dx may be dy. ws: a workspace of
     qk_norm_rope_workspace bytes (None: from torch's allocator)."""
-    where = "qk_norm_rope_backward"
     s = _qk_shapes(x, q_heads, k_heads, seq, q_gain is not None or k_gain is not None, eps, freq, pairs)
-    xp, ldx = _mat(x, *x.shape, x, where + " x")
-    gp, ldg = _mat(dy, *x.shape, x, where + " dy")
-    dp, ldd = _mat(dx, *x.shape, x, where + " dx")
-    gq, gk, pp, fp = _qk_params(s, x, q_gain, k_gain, pos, freq, where)
     dh = (s.head_dim,)
-    wq, wk = (_vec(t, dh, torch.float32, x, where + " gain gradient") for t in (g_q_gain, g_k_gain))
-    wb = _vec(g_bias, (x.shape[1],), torch.float32, x, where + " g_bias")
     ws, n = _workspace(ws, lib.paci_qk_norm_rope_workspace, s, x)
-    _launch(lib.paci_qk_norm_rope_backward, x, ctypes.byref(s), xp, ldx, gp, ldg, gq, gk, pp, fp, dp, ldd, wq, wk, wb,
-            ctypes.c_void_p(ws.data_ptr()), n)
+    _launch(lib.paci_qk_norm_rope_backward, x, ctypes.byref(s), _mat(x, x.shape, x, "qk_norm_rope x"), x.stride(0),
+            _mat(dy, x.shape, x, "qk_norm_rope dy"), dy.stride(0), _vec(q_gain, dh, _F32, x, "q_gain"),
+            _vec(k_gain, dh, _F32, x, "k_gain"), _vec(pos, (s.tokens,), _I32, x, "pos"),
+            _vec(freq, (s.rope_dims // 2,), _F64, x, "freq"), _mat(dx, x.shape, x, "qk_norm_rope dx"), dx.stride(0),
+            _vec(g_q_gain, dh, _F32, x, "g_q_gain"), _vec(g_k_gain, dh, _F32, x, "g_k_gain"),
+            _vec(g_bias, (x.shape[1],), _F32, x, "g_bias"), ws.data_ptr(), n)
     return dx
 
 
-def _attn_shapes(q, batch, n_heads, table=None, max_distance=0):
-    where = "attention"
-    dt = _operand(q, where)
-    if batch < 0 or n_heads < 1 or q.shape[1] % n_heads or (q.shape[0] % batch if batch else q.shape[0]):
-        raise PaciError(E_INVAL, f"{where}: {tuple(q.shape)} is not {batch} sequences of {n_heads} heads")
-    return PaciAttnShapes(dtype=dt, batch=batch, seq=q.shape[0] // batch if batch else 0, n_heads=n_heads,
-                          head_dim=q.shape[1] // n_heads, n_buckets=0 if table is None else table.shape[0],
-                          max_distance=max_distance)
-
-
-def _attn_operands(s, q, k, v, table, bounds, where):
+def _attn_shapes(q, batch, n_heads, table, max_distance):
+    dt = _operand(q, "attention q")
     T, d = q.shape
-    out = []
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        out += _mat(t, T, d, q, f"{where} {name}")
-    out.append(_vec(table, (s.n_buckets, s.n_heads), torch.float32, q, where + " table"))
-    out.append(_vec(bounds, (s.n_buckets,), torch.int32, q, where + " bounds"))
-    return out
+    if batch < 0 or n_heads < 1 or d % n_heads or (T % batch if batch else T):
+        _refuse(f"attention: {(T, d)} is not {batch} sequences of {n_heads} heads")
+    return PaciAttnShapes(dt, batch, T // batch if batch else 0, n_heads, d // n_heads, 0 if table is None else table.shape[0],
+                          max_distance)
 
 
-def _dense(t, like, where):
-    p, ld = _mat(t, *like.shape, like, where)
-    if ld != like.shape[1] and like.shape[0] > 1:
-        raise PaciError(E_INVAL, f"{where}: dense rows expected")
-    return p
+def _attn_inputs(s, q, k, v, table, bounds):
+    shape = q.shape
+    return (_mat(q, shape, q, "attention q"), q.stride(0), _mat(k, shape, q, "attention k"), k.stride(0),
+            _mat(v, shape, q, "attention v"), v.stride(0), _vec(table, (s.n_buckets, s.n_heads), _F32, q, "table"),
+            _vec(bounds, (s.n_buckets,), _I32, q, "bounds"))
 
 
 def attention(q, k, v, o, lse2, batch, n_heads, table=None, bounds=None, max_distance=0):
     """paci_attn_forward: causal attention of q, k and v [batch * seq, n_heads * head_dim]
-    into o (dense) and lse2 [batch * n_heads, seq] float32, with the relative position
+    into o (contiguous) and lse2 [batch * n_heads, seq] float32, with the relative position
     bias table [n_buckets, n_heads] float32 and its bounds [n_buckets] int32 (rel_bounds
     gives the usual ones), or without."""
-    where = "attention"
     s = _attn_shapes(q, batch, n_heads, table, max_distance)
-    ops = _attn_operands(s, q, k, v, table, bounds, where)
-    op = _dense(o, q, where + " o")
-    lp = _vec(lse2, (batch * n_heads, s.seq), torch.float32, q, where + " lse2")
-    _launch(lib.paci_attn_forward, q, ctypes.byref(s), *ops, op, lp)
+    _launch(lib.paci_attn_forward, q, ctypes.byref(s), *_attn_inputs(s, q, k, v, table, bounds),
+            _vec(o, q.shape, q.dtype, q, "o"), _vec(lse2, (batch * n_heads, s.seq), _F32, q, "lse2"))
     return o
+
+
+def attention_workspace(q, batch, n_heads, table=None, max_distance=0):
+    """Bytes of workspace that attention_backward needs for these operands."""
+    return _bytes(lib.paci_attn_workspace, _attn_shapes(q, batch, n_heads, table, max_distance))
 
 
 def attention_backward(q, k, v, o, lse2, do, dq, dk, dv, batch, n_heads, table=None, bounds=None, max_distance=0,
                        g_table=None, ws=None):
-    """paci_attn_backward: dq, dk and dv from do (dense like o) and the forward's operands, o
-    and lse2; g_table (float32, optional) is added to. ws: a workspace of
+    """paci_attn_backward: dq, dk and dv from do (contiguous like o) and the forward's operands,
+    o and lse2; g_table (float32, optional) is added to. ws: a workspace of
     attention_workspace bytes (None: from torch's allocator)."""
-    where = "attention_backward"
     s = _attn_shapes(q, batch, n_heads, table, max_distance)
-    ops = _attn_operands(s, q, k, v, table, bounds, where)
-    op, gp = _dense(o, q, where + " o"), _dense(do, q, where + " do")
-    lp = _vec(lse2, (batch * n_heads, s.seq), torch.float32, q, where + " lse2")
-    grads = []
-    for name, t in (("dq", dq), ("dk", dk), ("dv", dv)):
-        grads += _mat(t, *q.shape, q, f"{where} {name}")
-    tp = _vec(g_table, (s.n_buckets, n_heads), torch.float32, q, where + " g_table")
+    shape = q.shape
     ws, n = _workspace(ws, lib.paci_attn_workspace, s, q)
-    _launch(lib.paci_attn_backward, q, ctypes.byref(s), *ops, op, lp, gp, *grads, tp, ctypes.c_void_p(ws.data_ptr()), n)
+    _launch(lib.paci_attn_backward, q, ctypes.byref(s), *_attn_inputs(s, q, k, v, table, bounds),
+            _vec(o, shape, q.dtype, q, "o"), _vec(lse2, (batch * n_heads, s.seq), _F32, q, "lse2"),
+            _vec(do, shape, q.dtype, q, "do"), _mat(dq, shape, q, "dq"), dq.stride(0), _mat(dk, shape, q, "dk"), dk.stride(0),
+            _mat(dv, shape, q, "dv"), dv.stride(0), _vec(g_table, (s.n_buckets, n_heads), _F32, q, "g_table"),
+            ws.data_ptr(), n)
     return dq, dk, dv
 
 

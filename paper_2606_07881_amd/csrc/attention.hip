@@ -78,15 +78,27 @@ template <bool BIAS> __device__ __forceinline__ float query_lse(float lse2) {
   return BIAS && lse2 == -INFINITY ? INFINITY : lse2;
 }
 
-// Builds vec for head h (every thread of the workgroup; NTH threads; ends in a barrier).
-template <int NTH, int DH> __device__ __forceinline__ void bias_build(float* vec, const BiasArgs& a, int h, int H) {
+// A thread's bucket (thread index; at most 256 buckets): loaded ahead of the wait that covers
+// the first tiles.
+struct BiasEntry {
+  float t;
+  int bound;
+};
+__device__ __forceinline__ BiasEntry bias_load(const BiasArgs& a, int h, int H) {
+  const int i = min((int)threadIdx.x, a.n_buckets - 1);
+  return {a.table[(int64_t)i * H + h], a.bounds[i]};
+}
+// Builds vec for the head of the entries (every thread of the workgroup; NTH >= 256 threads;
+// ends in a barrier).
+template <int NTH, int DH> __device__ __forceinline__ void bias_build(float* vec, const BiasArgs& a, const BiasEntry& e) {
+  static_assert(NTH >= MAX_BUCKETS, "a thread per bucket");
   int* bnd = reinterpret_cast<int*>(vec + bias_len(a.max_distance));
   float* col = vec + bias_len(a.max_distance) + a.n_buckets;
-  for (int i = threadIdx.x; i < a.n_buckets; i += NTH) {
-    const float t = a.table[(int64_t)i * H + h];
-    bnd[i] = a.bounds[i];
+  if ((int)threadIdx.x < a.n_buckets) {
+    const float t = e.t * sqrtf((float)DH);
+    bnd[threadIdx.x] = e.bound;
     // entries so large that the product is not finite count as the largest number
-    col[i] = t <= BIAS_MASKED ? -INFINITY : t > 0.f ? fminf(t * sqrtf((float)DH), 3.4028235e38f) : t * sqrtf((float)DH);
+    col[threadIdx.x] = e.t <= BIAS_MASKED ? -INFINITY : t > 0.f ? fminf(t, 3.4028235e38f) : t;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < bias_len(a.max_distance); i += NTH) {
@@ -214,7 +226,7 @@ __global__ void __launch_bounds__(NT) attn_fwd_kernel(QkvView<T> in, T* out, flo
     const int kv = s * 4 + (l >> 4);
     qf[s] = (qrow < S) ? ld16(Qp + (int64_t)qrow * in.ldq + kv * V) : u32x4{0, 0, 0, 0};
   }
-  if constexpr (BIAS) bias_build<NT, DH>(bvec, bias, h, H);
+  if constexpr (BIAS) bias_build<NT, DH>(bvec, bias, bias_load(bias, h, H));
   floatx4 acc[DH / 16];
 #pragma unroll
   for (int t = 0; t < DH / 16; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -592,6 +604,8 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
     pv(kb, pf);
   };
 
+  BiasEntry entry{};
+  if constexpr (BIAS) entry = bias_load(bias, h, H);
 #pragma unroll
   for (int t = 0; t < NS - 1; ++t)
     if (t < nkb) fill(t);
@@ -601,7 +615,7 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   // loop, which would also wait for the ring's prefetches
   wait_vmcnt_all();
   if constexpr (BIAS) {
-    bias_build<C::NTF, DH>(bvec, bias, h, H);
+    bias_build<C::NTF, DH>(bvec, bias, entry);
     far = bias_far(bvec, bias.max_distance, scale_log2);
   }
   barrier_no_fence();
@@ -699,7 +713,7 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(QkvView<T> in, const 
     kf[s] = (key < S) ? ld16(Kp + (int64_t)key * in.ldk + kv * V) : u32x4{0, 0, 0, 0};
     vf[s] = (key < S) ? ld16(Vp + (int64_t)key * in.ldv + kv * V) : u32x4{0, 0, 0, 0};
   }
-  if constexpr (BIAS) bias_build<NT, DH>(bvec, bias, h, H);
+  if constexpr (BIAS) bias_build<NT, DH>(bvec, bias, bias_load(bias, h, H));
   floatx4 adk[DH / 16], adv[DH / 16];
 #pragma unroll
   for (int t = 0; t < DH / 16; ++t) adk[t] = adv[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -805,7 +819,7 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(QkvView<T> in, const T*
     diag.init(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets,
               bias.part != nullptr && qw0 < S ? bias.part + (((int64_t)h * bias.batch + b) * nrow + qw0 / 16) * (bias.max_distance + 1) : nullptr,
               bias.max_distance);
-    bias_build<NT, DH>(bvec, bias, h, H);
+    bias_build<NT, DH>(bvec, bias, bias_load(bias, h, H));
   }
   floatx4 adq[DH / 16];
 #pragma unroll
@@ -1018,13 +1032,15 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
     blk_fill<CPR, C::NTB>(dOp + (int64_t)q0 * d, d, S - q0, st + C::BLK * 16, wu, l);
     if (wu == 0 && l < C::PAIR_SLOTS) dma16(Pp + (int64_t)q0 * 2 + l * 4, st + 2 * C::BLK * 16);
   };
+  BiasEntry entry{};
+  if constexpr (BIAS) entry = bias_load(bias, h, H);
 #pragma unroll
   for (int t = 0; t < NS - 1; ++t)
     if (t < njobs) fill(t);
   wait_vmcnt_all();   // kf and vf known complete: no vmcnt(0) inside the loop
   FarValue far{0.f, 0};
   if constexpr (BIAS) {
-    bias_build<C::NTB, DH>(bvec, bias, h, H);
+    bias_build<C::NTB, DH>(bvec, bias, entry);
     far = bias_far(bvec, bias.max_distance, scale_log2);
   }
   for (int j = 0; j < njobs; ++j) {
@@ -1213,6 +1229,8 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
     blk_fill<CPR, C::NTB>(Kp + (int64_t)k0 * in.ldk, in.ldk, S - k0, st, wu, l);
     blk_fill<CPR, C::NTB>(Vp + (int64_t)k0 * in.ldv, in.ldv, S - k0, st + C::BLK * 16, wu, l);
   };
+  BiasEntry entry{};
+  if constexpr (BIAS) entry = bias_load(bias, h, H);
 #pragma unroll
   for (int t = 0; t < NS - 1; ++t)
     if (t < nkb) fill(t);
@@ -1225,7 +1243,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
     sums.init(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets,
               bias.part != nullptr && qw0 < S ? bias.part + (((int64_t)h * bias.batch + b) * nrow + qw0 / C::WR) * (bias.max_distance + 1) : nullptr,
               bias.max_distance);
-    bias_build<C::NTB, DH>(bvec, bias, h, H);
+    bias_build<C::NTB, DH>(bvec, bias, entry);
     far = bias_far(bvec, bias.max_distance, scale_log2);
   }
   for (int kb = 0; kb < nkb; ++kb) {
