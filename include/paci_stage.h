@@ -375,13 +375,14 @@ int paci_qk_norm_rope_backward(const paci_qk_shapes* s, const void* dev_x, int64
  *   o = softmax(q k^T / sqrt(head_dim) + table[bucket(i - j)][head]) v
  * over the keys j at or before each query i. bucket(n) is the number of
  * bounds[1 .. n_buckets - 1] at or below min(n, max_distance). Table entries at
- * or below -1e30 (-inf, the lowest float) hide their distances from that head;
+ * or below -1e9 (-inf, the lowest float) hide their distances from that head;
  * a query with no key left has o = 0 and lse2 = -inf and passes no gradient on.
+ * Finite entries above 1e9 count as 1e9.
  * n_buckets = 0: no bias (table, bounds and their gradient NULL). */
 typedef struct paci_attn_shapes {
   int32_t dtype;        /* enum paci_dtype, of q, k, v, o and their gradients */
   int32_t batch, seq;   /* token t = b * seq + s (either 0: the call does nothing) */
-  int32_t n_heads;      /* batch * n_heads at most 65535, seq at most 2^20 */
+  int32_t n_heads;      /* batch * n_heads at most 65535, seq at most 2^20, q at most 2^33 elements */
   int32_t head_dim;     /* 32, 64 or (bf16) 128 */
   int32_t n_buckets;    /* 0, or 2 .. 256 */
   int32_t max_distance; /* 1 .. 512: distances from it on are one */
@@ -400,7 +401,7 @@ int paci_rel_bounds(int n_buckets, int max_distance, int32_t* host_bounds);
  * not read as a bound). dev_o: [batch * seq, n_heads * head_dim], dense.
  * dev_lse2: fp32 [batch * n_heads, seq], log2 of the sum of 2^(score * log2 e).
  * Without a bias lse2 sums the probabilities as the products use them (rounded
- * to the dtype). Errors as for the norms. */
+ * to the dtype). dev_o must not be an operand. Errors as for the norms. */
 int paci_attn_forward(const paci_attn_shapes* s, const void* dev_q, int64_t ld_q, const void* dev_k, int64_t ld_k,
                       const void* dev_v, int64_t ld_v, const float* dev_table, const int32_t* dev_bounds, void* dev_o,
                       float* dev_lse2, void* hip_stream);
@@ -410,7 +411,7 @@ int paci_attn_forward(const paci_attn_shapes* s, const void* dev_q, int64_t ld_q
  * dq = dS k / sqrt(head_dim), dk = dS^T q / sqrt(head_dim), dv = P^T do, and
  * dev_g_table[b][h] (fp32 [n_buckets, n_heads], nullable) += the sum of dS over
  * the pairs of bucket b. dq, dk and dv have row strides and must not overlap an
- * operand. dev_ws: paci_attn_workspace bytes, 16-byte aligned. Errors as above. */
+ * operand or each other. dev_ws: paci_attn_workspace bytes, 16-byte aligned. Errors as above. */
 int paci_attn_workspace(const paci_attn_shapes* s, size_t* bytes);
 int paci_attn_backward(const paci_attn_shapes* s, const void* dev_q, int64_t ld_q, const void* dev_k, int64_t ld_k,
                        const void* dev_v, int64_t ld_v, const float* dev_table, const int32_t* dev_bounds,

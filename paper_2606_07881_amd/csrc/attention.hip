@@ -54,7 +54,9 @@ template <typename T> struct GradView {
 // A tile of 16 queries and 16 keys at distance 16 D holds distances 16 D - 15 .. 16 D + 15,
 // so tiles of equal D read the same values, and a block whose distances all reach
 // max_distance reads none: one value serves it (`far`).
-// Entries at or below MASKED hide their distances (-inf).
+// Entries at or below HIDDEN hide their distances (-inf), larger ones than MOST count as it:
+// the running maximum m of a row is rounded, so its largest exponent can be off zero by
+// 2^-24 |m|, which cancels in the quotient as long as 2 to that power is a float.
 struct BiasArgs {
   const float* table;      // [n_buckets][H]
   const int32_t* bounds;   // first distance of every bucket, ascending
@@ -63,7 +65,7 @@ struct BiasArgs {
   float* part;             // dQ wavefronts: sums of dS by distance, [H][batch][wavefront][max_distance + 1], or null
 };
 constexpr int BIAS_FRONT = 80, BIAS_TAIL = 128;   // distances below 0 (masked keys) and above max_distance inside a window
-constexpr float BIAS_MASKED = -1e30f;
+constexpr float BIAS_HIDDEN = -1e9f, BIAS_MOST = 1e9f;
 __host__ __device__ __forceinline__ int bias_len(int max_distance) { return BIAS_FRONT + max_distance + BIAS_TAIL; }
 // A dQ wavefront of SUB query tiles moves its diagonal sums through 4 rows of DiagRow floats of LDS.
 template <int SUB> struct DiagRow { static constexpr int N = 16 * (SUB + 5), FLOATS = 4 * N; };
@@ -95,10 +97,9 @@ template <int NTH, int DH> __device__ __forceinline__ void bias_build(float* vec
   int* bnd = reinterpret_cast<int*>(vec + bias_len(a.max_distance));
   float* col = vec + bias_len(a.max_distance) + a.n_buckets;
   if ((int)threadIdx.x < a.n_buckets) {
-    const float t = e.t * sqrtf((float)DH);
+    const float t = (e.t > BIAS_MOST && e.t < INFINITY ? BIAS_MOST : e.t) * sqrtf((float)DH);
     bnd[threadIdx.x] = e.bound;
-    // entries so large that the product is not finite count as the largest number
-    col[threadIdx.x] = e.t <= BIAS_MASKED ? -INFINITY : t > 0.f ? fminf(t, 3.4028235e38f) : t;
+    col[threadIdx.x] = e.t <= BIAS_HIDDEN ? -INFINITY : t;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < bias_len(a.max_distance); i += NTH) {

@@ -15,7 +15,7 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) &
 // Rows of `cols` elements with stride ld (elements): 16-byte aligned, not overlapping.
 bool rows_ok(const void* p, int64_t ld, int64_t cols, int64_t rows, int dtype) {
   const int64_t vec = dtype == PACI_BF16 ? 8 : 4;
-  return p && aligned(p, 16) && ld % vec == 0 && (ld >= cols || (rows <= 1 && ld >= 0)) && ld <= (1LL << 40);
+  return p && aligned(p, 16) && ld % vec == 0 && (ld >= cols || (rows <= 1 && ld >= 0)) && ld <= (1LL << 46) / rows;
 }
 bool floats_ok(const float* p) { return p && aligned(p, 4); }
 
@@ -69,7 +69,8 @@ int check_attn(const paci_attn_shapes* s) {
   if ((dh != 32 && dh != 64 && dh != 128) || (s->dtype == PACI_FP32 && dh == 128)) return PACI_E_UNSUPPORTED;
   if (s->n_buckets > paci::MAX_BUCKETS || (s->n_buckets && s->max_distance > paci::MAX_DISTANCE)) return PACI_E_UNSUPPORTED;
   // launch grids: one workgroup column per (sequence, head), rows of at least 64 queries
-  if ((int64_t)s->batch * s->n_heads > 65535 || s->seq > (1 << 20) || (int64_t)s->batch * s->seq > (1 << 30))
+  if ((int64_t)s->batch * s->n_heads > 65535 || s->seq > (1 << 20) || (int64_t)s->batch * s->seq > (1 << 30) ||
+      (int64_t)s->batch * s->n_heads * s->seq * dh > (1LL << 33))
     return PACI_E_UNSUPPORTED;
   return PACI_OK;
 }
@@ -192,6 +193,7 @@ extern "C" int paci_attn_forward(const paci_attn_shapes* s, const void* dev_q, i
   if (!rows_ok(dev_q, ld_q, d, T, s->dtype) || !rows_ok(dev_k, ld_k, d, T, s->dtype) ||
       !rows_ok(dev_v, ld_v, d, T, s->dtype) || !rows_ok(dev_o, d, d, T, s->dtype) || !floats_ok(dev_lse2))
     return PACI_E_INVAL;
+  if (dev_o == dev_q || dev_o == dev_k || dev_o == dev_v) return PACI_E_INVAL;   // other workgroups still read them
   if (s->n_buckets ? !floats_ok(dev_table) || !dev_bounds || !aligned(dev_bounds, 4) : dev_table || dev_bounds)
     return PACI_E_INVAL;
   paci::AttnArgs a = attn_shape_args(*s);
@@ -235,6 +237,7 @@ extern "C" int paci_attn_backward(const paci_attn_shapes* s, const void* dev_q, 
   for (const void* out : {(const void*)dev_dq, (const void*)dev_dk, (const void*)dev_dv})
     for (const void* in : {dev_q, dev_k, dev_v, dev_o, dev_do})
       if (out == in) return PACI_E_INVAL;
+  if (dev_dq == dev_dk || dev_dq == dev_dv || dev_dk == dev_dv) return PACI_E_INVAL;
   if (s->n_buckets ? !floats_ok(dev_table) || !dev_bounds || !aligned(dev_bounds, 4) : dev_table || dev_bounds || dev_g_table)
     return PACI_E_INVAL;
   if (!aligned(dev_g_table, 4) || !dev_ws || !aligned(dev_ws, 16)) return PACI_E_INVAL;

@@ -241,6 +241,7 @@ class Attn:
                 t[g.random(t.shape) < 0.3] = -np.inf
             elif hidden == "lowest":
                 t[g.random(t.shape) < 0.5] = np.finfo(np.float32).min
+                t[g.random(t.shape) < 0.2] = -1e9
             self.bias = positions.bias_by_distance(t, self.bounds, md, self.S)
         qkv = np.concatenate([self.q, self.k, self.v], 1)
         self.o, lse = model.attention_fwd(qkv, self.B, self.S, self.H, self.dh, bias=self.bias)
@@ -346,3 +347,62 @@ def test_attention_without_tokens(binding):
     for batch in (0, 2):
         lse2 = torch.empty(batch, 0, device="cuda")
         binding.attention(x, x, x, x, lse2, batch, 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("entry", [1e8, 3e38])
+def test_attention_with_an_entry_beyond_every_score(binding, dtype, entry):
+    """One distance outweighs all others in every head: each query returns the value that far back, the first ones
+    what they would without it; the gradient of that query's scores vanishes and everything stays finite."""
+    import torch
+    B, S, H, dh, far = 2, 140, 2, 64, 3
+    c = Attn((B, S, H, dh, 8, 7, ""), dtype, 6)
+    c.bounds = np.arange(8, dtype=np.int32)   # a bucket per distance
+    c.table[far] = entry
+    (q, k, v), kw = c.device()
+    o, lse2 = torch.empty(c.T, c.d, device="cuda", dtype=q.dtype), torch.empty(B * H, S, device="cuda")
+    binding.attention(q, k, v, o, lse2, **kw)
+    got, val = c.split(host(o)), c.split(c.v)
+    # the one probability left is 2^e, e the rounding of a running maximum near 1e8 (not 0): in bf16 it is rounded
+    # to 2^e (1 + u) before its product, against 2^e in the normaliser, and the output is rounded: (1 + u)^2 - 1.
+    # In fp32: 1 / l, its product and the output, and the error of 2^e cancels
+    u = half_step(dtype)
+    check(got[:, :, far:], val[:, :, :-far], ((2.01 * u if dtype == "bf16" else u) + 4 * U32) * np.abs(val[:, :, :-far]), "o")
+    assert torch.isfinite(lse2).all()
+    grads = [torch.empty(c.T, c.d, device="cuda", dtype=q.dtype) for _ in range(3)]
+    g_table = torch.zeros(8, H, device="cuda")
+    binding.attention_backward(q, k, v, o, lse2, dev(c.do, dtype), *grads, g_table=g_table, **kw)
+    assert all(torch.isfinite(t).all() for t in grads + [g_table])
+
+
+def test_first_call_of_a_process_can_be_captured(binding, root):
+    """A fresh process whose first device work of this library is under capture."""
+    import subprocess
+    import sys
+    code = """
+import sys
+sys.path.insert(0, {root!r})
+import torch
+from paper_2606_07881_amd import binding
+x = torch.randn(64, 192, device="cuda")
+y, o, l = torch.empty(64, 128, device="cuda"), torch.empty(64, 64, device="cuda"), torch.empty(2, 32, device="cuda")
+g, t = torch.ones(32, device="cuda"), torch.zeros(8, 2, device="cuda")
+b = torch.from_numpy(binding.rel_bounds(8, 20)).cuda()
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+def chain():
+    binding.qk_norm_rope(x[:, :128], y, 2, 2, seq=32, q_gain=g, k_gain=g)
+    binding.attention(y[:, :64], y[:, 64:], x[:, 128:], o, l, 2, 2, t, b, 20)
+with torch.cuda.graph(graph):
+    chain()
+for _ in range(3):
+    x.normal_()
+    graph.replay()
+    a = o.clone()
+    chain()
+    torch.cuda.synchronize()
+    assert torch.equal(a, o)
+print("replays agree")
+""".format(root=root)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and "replays agree" in r.stdout, r.stdout + r.stderr

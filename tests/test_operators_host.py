@@ -71,7 +71,7 @@ def test_qk_shapes_are_refused(over, code):
 def test_qk_buffers_are_refused():
     s = binding.PaciQkShapes(**QK)
     for over in [dict(x=None), dict(x=A + 8), dict(ldx=255), dict(ldx=252), dict(ldx=248), dict(ldx=-256), dict(gq=None),
-                 dict(gk=None), dict(gq=A + 2), dict(pos=A + 2), dict(freq=None), dict(freq=A + 4), dict(ldx=2 ** 41)]:
+                 dict(gk=None), dict(gq=A + 2), dict(pos=A + 2), dict(freq=None), dict(freq=A + 4), dict(ldx=2 ** 45)]:
         assert qk_fwd(s, **over) == INVAL, over
         assert qk_bwd(s, **over) == INVAL, over
     for over in [dict(y=None), dict(y=2 * A + 4), dict(ldy=128), dict(y=A, ldy=264)]:
@@ -94,7 +94,7 @@ ATTN_BAD = [
     (dict(n_buckets=-1), INVAL), (dict(n_buckets=1), INVAL), (dict(max_distance=0), INVAL), (dict(dtype=2), UNSUP),
     (dict(head_dim=48), UNSUP), (dict(head_dim=128, dtype=0), UNSUP), (dict(n_buckets=257), UNSUP),
     (dict(max_distance=513), UNSUP), (dict(batch=32768, n_heads=2), UNSUP), (dict(seq=2 ** 20 + 1), UNSUP),
-    (dict(batch=2048, seq=2 ** 20, n_heads=1), UNSUP), (dict(batch=2 ** 31 - 1, n_heads=2 ** 31 - 1), UNSUP),
+    (dict(batch=2048, seq=2 ** 20, n_heads=1), UNSUP), (dict(batch=256, seq=2 ** 20, n_heads=1), UNSUP), (dict(batch=2 ** 31 - 1, n_heads=2 ** 31 - 1), UNSUP),
 ]
 
 
@@ -126,12 +126,12 @@ def test_attention_buffers_are_refused():
     s = binding.PaciAttnShapes(**ATTN)
     both = [dict(zip((n, "ld" + n), bad)) for n in "qkv" for bad in ((None, 128), (A + 8, 128), (A, 120), (A, 132), (A, -128))]
     both += [dict(table=None), dict(bounds=None), dict(table=A + 2), dict(bounds=A + 2), dict(o=None), dict(o=A + 8),
-             dict(lse2=None), dict(lse2=A + 2)]
+             dict(lse2=None), dict(lse2=A + 2), dict(o=A), dict(q=A, ldq=2 ** 41)]
     for over in both:
         assert attn_fwd(s, **over) == INVAL, over
         assert attn_bwd(s, **over) == INVAL, over
     for over in [dict(do=None), dict(do=A + 8), dict(dq=None), dict(dk=None), dict(dv=None), dict(lddq=64), dict(lddk=64),
-                 dict(lddv=132), dict(dq=A), dict(dk=A), dict(dv=A), dict(dv=3 * A), dict(dq=5 * A), dict(gt=A + 2), dict(ws=None),
+                 dict(lddv=132), dict(dq=A), dict(dk=A), dict(dv=A), dict(dv=3 * A), dict(dq=5 * A), dict(dq=4 * A), dict(dv=2 * A), dict(dk=6 * A), dict(gt=A + 2), dict(ws=None),
                  dict(ws=A + 8)]:
         assert attn_bwd(s, **over) == INVAL, over
     n = ctypes.c_size_t(0)
