@@ -385,7 +385,7 @@ sys.path.insert(0, {root!r})
 import torch
 from paper_2606_07881_amd import binding
 x = torch.randn(64, 192, device="cuda")
-y, o, l = torch.empty(64, 128, device="cuda"), torch.empty(64, 64, device="cuda"), torch.empty(2, 32, device="cuda")
+y, o, l = torch.empty(64, 128, device="cuda"), torch.empty(64, 64, device="cuda"), torch.empty(4, 32, device="cuda")
 g, t = torch.ones(32, device="cuda"), torch.zeros(8, 2, device="cuda")
 b = torch.from_numpy(binding.rel_bounds(8, 20)).cuda()
 torch.cuda.synchronize()

@@ -126,10 +126,11 @@ def test_attention_buffers_are_refused():
     s = binding.PaciAttnShapes(**ATTN)
     both = [dict(zip((n, "ld" + n), bad)) for n in "qkv" for bad in ((None, 128), (A + 8, 128), (A, 120), (A, 132), (A, -128))]
     both += [dict(table=None), dict(bounds=None), dict(table=A + 2), dict(bounds=A + 2), dict(o=None), dict(o=A + 8),
-             dict(lse2=None), dict(lse2=A + 2), dict(o=A), dict(q=A, ldq=2 ** 41)]
+             dict(lse2=None), dict(lse2=A + 2), dict(q=A, ldq=2 ** 41)]
     for over in both:
         assert attn_fwd(s, **over) == INVAL, over
         assert attn_bwd(s, **over) == INVAL, over
+    assert attn_fwd(s, o=A) == INVAL   # an operand
     for over in [dict(do=None), dict(do=A + 8), dict(dq=None), dict(dk=None), dict(dv=None), dict(lddq=64), dict(lddk=64),
                  dict(lddv=132), dict(dq=A), dict(dk=A), dict(dv=A), dict(dv=3 * A), dict(dq=5 * A), dict(dq=4 * A), dict(dv=2 * A), dict(dk=6 * A), dict(gt=A + 2), dict(ws=None),
                  dict(ws=A + 8)]:
