@@ -52,8 +52,10 @@ template <typename T> struct GradView {
 // The products of a tile start from it instead of from zero (the matrix instruction's
 // third operand), so adding it costs no vector instruction.
 // A tile of 16 queries and 16 keys at distance 16 D holds distances 16 D - 15 .. 16 D + 15,
-// so tiles of equal D read the same values, and a block whose distances all reach
-// max_distance reads none: one value serves it (`far`).
+// so tiles of equal D read the same values. A block whose distances all reach max_distance
+// reads the last value everywhere; a path of its own for such blocks, with the one value in
+// the exponent's constant, was no faster (backward 116 against 113 us at 8 x 1024 tokens, 16
+// heads of 64; 385 against 372 at 4 x 2048, 16 heads of 128, max_distance 256).
 // Entries at or below HIDDEN hide their distances (-inf), larger ones than MOST count as it:
 // the running maximum m of a row is rounded, so its largest exponent can be off zero by
 // 2^-24 |m|, which cancels in the quotient as long as 2 to that power is a float.
@@ -113,18 +115,6 @@ template <int NTH, int DH> __device__ __forceinline__ void bias_build(float* vec
     vec[i] = col[lo];
   }
   __syncthreads();
-}
-
-// The value of a block whose distances all reach max_distance, in units of log 2, and the
-// least distance of a block from which it serves: max_distance, or never where adding it to
-// the exponent is not the same as adding it to the score (a hidden, NaN or huge entry).
-struct FarValue {
-  float b;
-  int from;
-};
-__device__ __forceinline__ FarValue bias_far(const float* vec, int max_distance, float scale_log2) {
-  const float b = scale_log2 * as_float(__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, vec[BIAS_FRONT + max_distance])));
-  return {b, fabsf(b) <= 1024.f ? max_distance : 0x7fffffff};
 }
 
 // Sums over the diagonals of dS, for the table's gradient: a dQ wavefront of 16 SUB
@@ -440,16 +430,12 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
     blk_fill<CPR, C::NTF>(Kp + (int64_t)k0 * in.ldk, in.ldk, S - k0, st, wu, l);
     blk_fill<CPR, C::NTF>(Vp + (int64_t)k0 * in.ldv, in.ldv, S - k0, st + C::BLK * 16, wu, l);
   };
-  // with a bias, whether block kb has distances below far.from, which read the vector
-  FarValue far{0.f, 0};
-  auto is_near = [&](int kb) { return BIAS && qw0 - kb * BKV - (BKV - 1) < far.from; };
-  // raw scores q k^T of key block kb, with its bias where it reads the vector
-  auto scores = [&](auto vec, int kb, floatx4 (&sc)[QS][4]) {
+  // raw scores q k^T of key block kb, with their bias
+  auto scores = [&](int kb, floatx4 (&sc)[QS][4]) {
     const u32x4* sK = ring + (kb % NS) * 2 * C::BLK;
-    const float* bp = decltype(vec)::value ? bvec + BIAS_FRONT + min(qw0 - kb * BKV, bias.max_distance + 63) + (l & 15) - 4 * g
-                                           : nullptr;
-    floatx4 b[QS + 3];   // of the tiles' distances qs - kt
-    if constexpr (decltype(vec)::value) {
+    floatx4 b[QS + 3];   // bias of the tiles' distances qs - kt
+    if constexpr (BIAS) {
+      const float* bp = bvec + BIAS_FRONT + min(qw0 - kb * BKV, bias.max_distance + 63) + (l & 15) - 4 * g;
 #pragma unroll
       for (int i = 0; i < QS + 3; ++i)
 #pragma unroll
@@ -462,7 +448,7 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
       for (int s = 0; s < KS; ++s) kf[s] = blk_frag<CPR>(sK, s, kt * 16);
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) {
-        if constexpr (decltype(vec)::value) sc[qs][kt] = b[qs - kt + 3];
+        if constexpr (BIAS) sc[qs][kt] = b[qs - kt + 3];
         else sc[qs][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < KS; ++s) mma_step<bf16>(sc[qs][kt], kf[s], qf[qs][s]);
@@ -471,8 +457,7 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   };
   // online softmax of block kb's scores: running max and sum, rescaled
   // accumulators, and the probabilities (dropped ones zeroed) as bf16 fragments
-  auto softmax = [&](auto masked, auto is_far, int kb, floatx4 (&sc)[QS][4], u32x4 (&pf)[QS][2]) {
-    constexpr bool FAR = decltype(is_far)::value;
+  auto softmax = [&](auto masked, int kb, floatx4 (&sc)[QS][4], u32x4 (&pf)[QS][2]) {
     const int k0 = kb * BKV;
 #pragma unroll
     for (int qs = 0; qs < QS; ++qs) {
@@ -492,14 +477,13 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
 #pragma unroll
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[qs][kt][r]);
       mx = group4_max(mx);
-      const float m_new = fmaxf(m_run[qs], FAR ? fmaf(mx, scale_log2, far.b) : mx * scale_log2);
+      const float m_new = fmaxf(m_run[qs], mx * scale_log2);
       const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
       const float alpha = fast_exp2(m_run[qs] - m_use);
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          sc[qs][kt][r] = fast_exp2(fmaf(sc[qs][kt][r], scale_log2, FAR ? far.b - m_use : -m_use));
+        for (int r = 0; r < 4; ++r) sc[qs][kt][r] = fast_exp2(fmaf(sc[qs][kt][r], scale_log2, -m_use));
       if constexpr (BIAS) {
         float rs = 0.f;
 #pragma unroll
@@ -567,9 +551,13 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
     if (kb + NS - 1 < nkb) fill(kb + NS - 1);
     if (kb > my_last) return;
     u32x4 pf[QS][2];
-    auto inner = [&](auto vec_next, auto is_far) {   // the next block's scores beside this one's softmax
-      scores(vec_next, kb + 1, nxt);
-      softmax(std::false_type{}, is_far, kb, cur, pf);
+    if constexpr (!PIPE) {
+      scores(kb, cur);
+      if (kb < my_last) softmax(std::false_type{}, kb, cur, pf);
+      else softmax(std::true_type{}, kb, cur, pf);
+    } else if (kb < my_last) {
+      scores(kb + 1, nxt);
+      softmax(std::false_type{}, kb, cur, pf);
       // interleave: the fragment reads first, then one MFMA per few ALU instructions
       __builtin_amdgcn_sched_group_barrier(0x100, 4 * KS, 0);
 #pragma unroll
@@ -577,30 +565,8 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
       }
-    };
-    using Y = std::true_type;
-    using N = std::false_type;
-    if constexpr (!PIPE) {
-      const bool near = is_near(kb);
-      if constexpr (BIAS) {
-        if (near) scores(Y{}, kb, cur);
-        else scores(N{}, kb, cur);
-      } else {
-        scores(N{}, kb, cur);
-      }
-      if (kb >= my_last) softmax(Y{}, N{}, kb, cur, pf);
-      else if (!BIAS || near) softmax(N{}, N{}, kb, cur, pf);
-      else softmax(N{}, Y{}, kb, cur, pf);
-    } else if (kb >= my_last) {
-      softmax(Y{}, N{}, kb, cur, pf);
-    } else if constexpr (!BIAS) {
-      inner(N{}, N{});
-    } else if (is_near(kb)) {   // key blocks come nearer: the next one is near too
-      inner(Y{}, N{});
-    } else if (is_near(kb + 1)) {
-      inner(Y{}, Y{});
     } else {
-      inner(N{}, Y{});
+      softmax(std::true_type{}, kb, cur, pf);
     }
     pv(kb, pf);
   };
@@ -615,19 +581,9 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
   // compiler sees: it then knows qf has landed and puts no vmcnt(0) in the
   // loop, which would also wait for the ring's prefetches
   wait_vmcnt_all();
-  if constexpr (BIAS) {
-    bias_build<C::NTF, DH>(bvec, bias, entry);
-    far = bias_far(bvec, bias.max_distance, scale_log2);
-  }
+  if constexpr (BIAS) bias_build<C::NTF, DH>(bvec, bias, entry);
   barrier_no_fence();
-  if (PIPE && my_last >= 0) {
-    if constexpr (BIAS) {
-      if (is_near(0)) scores(std::true_type{}, 0, sA);
-      else scores(std::false_type{}, 0, sA);
-    } else {
-      scores(std::false_type{}, 0, sA);
-    }
-  }
+  if (PIPE && my_last >= 0) scores(0, sA);
   for (int kb = 0; kb < nkb; kb += 2) {
     step(kb, sA, sB);
     if (kb + 1 < nkb) step(kb + 1, sB, sA);
@@ -1039,11 +995,7 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
   for (int t = 0; t < NS - 1; ++t)
     if (t < njobs) fill(t);
   wait_vmcnt_all();   // kf and vf known complete: no vmcnt(0) inside the loop
-  FarValue far{0.f, 0};
-  if constexpr (BIAS) {
-    bias_build<C::NTB, DH>(bvec, bias, entry);
-    far = bias_far(bvec, bias.max_distance, scale_log2);
-  }
+  if constexpr (BIAS) bias_build<C::NTB, DH>(bvec, bias, entry);
   for (int j = 0; j < njobs; ++j) {
     wait_loads<C::L, NS - 2>(min(njobs - 1, j + NS - 2) - j);
     wait_lds_reads();
@@ -1058,20 +1010,15 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
     const bool edge = (q0 < kw0 + C::WR - 1) || (q0 + 64 > S) || (kw0 + C::WR > S);
     // the bias of query 16 t + 4 g + r and key 16 ks + l % 16 of these: bp[16 (t - ks) + r]
     const float* bp = BIAS ? bvec + BIAS_FRONT + min(q0 - kw0, bias.max_distance + C::WR - 1) + 4 * g - (l & 15) : nullptr;
-    const bool near = BIAS && (edge || q0 - kw0 - (C::WR - 1) < far.from);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {   // 32 queries: tiles 2s and 2s + 1
       floatx4 sc[SUB][2], dp[SUB][2];
-      floatx4 bv[SUB + 1];   // bias of the tiles' distances 2 s + u - ks (0 in a far block)
+      floatx4 bv[SUB + 1];   // bias of the tiles' distances 2 s + u - ks
       if constexpr (BIAS) {
 #pragma unroll
-        for (int i = 0; i <= SUB; ++i) bv[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-        if (near) {
+        for (int i = 0; i <= SUB; ++i)
 #pragma unroll
-          for (int i = 0; i <= SUB; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) bv[i][r] = bp[16 * (2 * s + i - SUB + 1) + r];
-        }
+          for (int r = 0; r < 4; ++r) bv[i][r] = bp[16 * (2 * s + i - SUB + 1) + r];
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -1096,13 +1043,13 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
       // Dropout M = keep * scale: dV takes P M, and dP = (dO V^T) M.
       uint32_t dbits[2][SUB];
       if constexpr (DROP) drop_col4_quad<SUB>(drop, bh, q0 + 32 * s, kw0, dbits);
-      auto softmax = [&](auto masked, auto is_far) {
+      auto softmax = [&](auto masked) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int qi = (2 * s + u) * 16 + 4 * g + r;
-            const float lq = decltype(is_far)::value ? sP[2 * qi] - far.b : sP[2 * qi], Dq = sP[2 * qi + 1];
+            const float lq = sP[2 * qi], Dq = sP[2 * qi + 1];
 #pragma unroll
             for (int ks = 0; ks < SUB; ++ks) {
               float x = fmaf(sc[ks][u][r], scale_log2, -lq);
@@ -1122,9 +1069,8 @@ __device__ __forceinline__ void dkdv_ring_body(u32x4* ring, float* bvec, int kb,
             }
           }
       };
-      if (edge) softmax(std::true_type(), std::false_type());
-      else if (!BIAS || near) softmax(std::false_type(), std::false_type());
-      else if constexpr (BIAS) softmax(std::false_type(), std::true_type());
+      if (edge) softmax(std::true_type());
+      else softmax(std::false_type());
       u32x4 pfr[SUB], dsf[SUB];
 #pragma unroll
       for (int ks = 0; ks < SUB; ++ks) {
@@ -1238,14 +1184,12 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
   wait_vmcnt_all();   // qf, gf, lq and Dq known complete: no vmcnt(0) inside the loop
   DiagSums<SUB> sums;
   float far_sum[4] = {0.f, 0.f, 0.f, 0.f};   // of dS over blocks beyond max_distance
-  FarValue far{0.f, 0};
   if constexpr (BIAS) {
     const int nrow = (S + C::WR - 1) / C::WR;
     sums.init(bvec + bias_len(bias.max_distance) + 2 * bias.n_buckets,
               bias.part != nullptr && qw0 < S ? bias.part + (((int64_t)h * bias.batch + b) * nrow + qw0 / C::WR) * (bias.max_distance + 1) : nullptr,
               bias.max_distance);
     bias_build<C::NTB, DH>(bvec, bias, entry);
-    far = bias_far(bvec, bias.max_distance, scale_log2);
   }
   for (int kb = 0; kb < nkb; ++kb) {
     wait_loads<C::L, NS - 2>(min(nkb - 1, kb + NS - 2) - kb);
@@ -1257,7 +1201,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
     const u32x4* sV = sK + C::BLK;
     const int k0 = kb * BKV;
     const bool edge = (k0 + BKV - 1 > qw0) || (k0 + BKV > S) || (qw0 + C::WR > S);
-    const bool near = !BIAS || edge || qw0 - k0 - (BKV - 1) < far.from;
+    const bool near = !BIAS || edge || qw0 - k0 - (BKV - 1) < bias.max_distance;   // dS goes to more than one distance
     const float* bp = BIAS ? bvec + BIAS_FRONT + min(qw0 - k0, bias.max_distance + 63) + (l & 15) - 4 * g : nullptr;
     float diag[SUB + 3][4];
     if constexpr (BIAS) {
@@ -1269,16 +1213,12 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
 #pragma unroll
     for (int s = 0; s < 2; ++s) {   // 32 keys: tiles 2s and 2s + 1
       floatx4 sc[SUB][2], dp[SUB][2];
-      floatx4 bv[SUB + 1];   // bias of the tiles' distances qs - 2 s - u (0 in a far block)
+      floatx4 bv[SUB + 1];   // bias of the tiles' distances qs - 2 s - u
       if constexpr (BIAS) {
 #pragma unroll
-        for (int i = 0; i <= SUB; ++i) bv[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-        if (near) {
+        for (int i = 0; i <= SUB; ++i)
 #pragma unroll
-          for (int i = 0; i <= SUB; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) bv[i][r] = bp[16 * (i - 1 - 2 * s) - r];
-        }
+          for (int r = 0; r < 4; ++r) bv[i][r] = bp[16 * (i - 1 - 2 * s) - r];
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -1303,7 +1243,6 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
         constexpr bool FAR = decltype(is_far)::value;
 #pragma unroll
         for (int qs = 0; qs < SUB; ++qs) {
-          const float lqb = FAR ? lq[qs] - far.b : lq[qs];
           const int q = qw0 + 16 * qs + (l & 15);
           uint32_t dbits[2] = {0xfu, 0xfu};   // dropout M = keep * scale on dP = dO V^T
           if constexpr (DROP) drop_row4_pair(drop, bh, q, k0 + 32 * s + 4 * g, k0 + 32 * s + 16 + 4 * g, dbits[0], dbits[1]);
@@ -1312,7 +1251,7 @@ __device__ __forceinline__ void dq_ring_body(u32x4* ring, float* bvec, int yb, c
             const uint32_t bits = dbits[u];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float x = fmaf(sc[qs][u][r], scale_log2, -lqb);
+              float x = fmaf(sc[qs][u][r], scale_log2, -lq[qs]);
               if constexpr (decltype(masked)::value) {
                 const int key = k0 + (2 * s + u) * 16 + 4 * g + r;
                 x = (key <= q && key < S && q < S) ? x : -INFINITY;
