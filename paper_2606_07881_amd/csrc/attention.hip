@@ -559,7 +559,8 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
       scores(kb + 1, nxt);
       softmax(std::false_type{}, kb, cur, pf);
       // interleave: the fragment reads first, then one MFMA per few ALU instructions
-      __builtin_amdgcn_sched_group_barrier(0x100, 4 * KS, 0);
+      // (with a bias its reads too: 133 against 140 us at 4 x 2048 tokens, 16 heads of 128)
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * KS + (BIAS ? 2 * (QS + 3) : 0), 0);
 #pragma unroll
       for (int i = 0; i < 4 * KS * QS; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -635,23 +636,29 @@ __global__ void __launch_bounds__(NT) attn_dsum_kernel(const T* o, const T* dO, 
 }
 
 // ---------------------------------------------------------------------------------------
+// The fp32 backward's two kinds of workgroup (tiles: BwdTiles<T, DH>::SLOTS slots of LDS).
+template <typename T, int DH> struct BwdTiles {
+  static constexpr int BQ = (DH >= 128) ? 32 : 64;   // queries per staged block of dK/dV (LDS budget)
+  static constexpr int TILE = DH / Vec<T>::V * 64;   // 64 rows of a head
+  static constexpr int DKDV = 4 * DH / Vec<T>::V * BQ + BQ / 2, DQ = 3 * TILE;
+  static constexpr int SLOTS = DKDV > DQ ? DKDV : DQ;
+};
 template <typename T, int DH, bool DROP, bool BIAS>
-__global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(QkvView<T> in, const T* dO, const float* lse2,
-                                                            const float* Dsum, GradView<T> grad, int S, int H, int d,
-                                                            float scale_log2, float scale, DropArgs drop, BiasArgs bias) {
-  extern __shared__ float bvec[];
+__device__ __forceinline__ void dkdv_body(u32x4* tiles, float* bvec, int kb, const QkvView<T>& in, const T* dO,
+                                          const float* lse2, const float* Dsum, const GradView<T>& grad, int S, int H, int d,
+                                          float scale_log2, float scale, const DropArgs& drop, const BiasArgs& bias) {
   constexpr int V = Vec<T>::V;
-  constexpr int BQ = (DH >= 128) ? 32 : 64;  // queries per staged block (LDS budget)
+  constexpr int BQ = BwdTiles<T, DH>::BQ;
   constexpr int DKV = DH / V;
   constexpr int QSTEPS = DH / (4 * V);
   constexpr int RSTEPS = BQ / (4 * V);       // MFMA steps over a query block
-  __shared__ u32x4 sQ[DKV * BQ];
-  __shared__ u32x4 sdO[DKV * BQ];
-  __shared__ u32x4 sQt[(BQ / V) * DH];
-  __shared__ u32x4 sdOt[(BQ / V) * DH];
-  __shared__ float sL[BQ], sD[BQ];
+  u32x4* sQ = tiles;
+  u32x4* sdO = sQ + DKV * BQ;
+  u32x4* sQt = sdO + DKV * BQ;
+  u32x4* sdOt = sQt + (BQ / V) * DH;
+  float* sL = reinterpret_cast<float*>(sdOt + (BQ / V) * DH);
+  float* sD = sL + BQ;
 
-  const int kb = blockIdx.x;
   const int bh = blockIdx.y, b = bh / H, h = bh % H;
   const int w = threadIdx.x >> 6, l = lane_id();
   const T* Qp = in.q + (int64_t)b * S * in.ldq + h * DH;
@@ -736,21 +743,20 @@ __global__ void __launch_bounds__(NT) attn_bwd_dkdv_kernel(QkvView<T> in, const 
 }
 
 template <typename T, int DH, bool DROP, bool BIAS>
-__global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(QkvView<T> in, const T* dO, const float* lse2,
-                                                          const float* Dsum, GradView<T> grad, int S, int H, int d,
-                                                          float scale_log2, float scale, DropArgs drop, BiasArgs bias) {
-  extern __shared__ float bvec[];
+__device__ __forceinline__ void dq_body(u32x4* tiles, float* bvec, int yb, const QkvView<T>& in, const T* dO,
+                                        const float* lse2, const float* Dsum, const GradView<T>& grad, int S, int H, int d,
+                                        float scale_log2, float scale, const DropArgs& drop, const BiasArgs& bias) {
   constexpr int V = Vec<T>::V;
   constexpr int BQ = 64;
   constexpr int DKV = DH / V;
   constexpr int QSTEPS = DH / (4 * V);
   constexpr int PSTEPS = BKV / (4 * V);
-  __shared__ u32x4 sK[DKV * BKV];
-  __shared__ u32x4 sV[DKV * BKV];
-  __shared__ u32x4 sKt[(BKV / V) * DH];
+  u32x4* sK = tiles;
+  u32x4* sV = sK + DKV * BKV;
+  u32x4* sKt = sV + DKV * BKV;
 
   const int nqb = (S + BQ - 1) / BQ;
-  const int qb = nqb - 1 - blockIdx.x;
+  const int qb = nqb - 1 - yb;
   const int bh = blockIdx.y, b = bh / H, h = bh % H;
   const int w = threadIdx.x >> 6, l = lane_id();
   const T* Qp = in.q + (int64_t)b * S * in.ldq + h * DH;
@@ -839,6 +845,21 @@ __global__ void __launch_bounds__(NT) attn_bwd_dq_kernel(QkvView<T> in, const T*
   if constexpr (BIAS) {
     if (diag.out != nullptr) diag.finish(q0 + 16 * w - last_kb * BKV);
   }
+}
+
+// dK/dV of key block x below nkb, then dQ (largest queries first): one launch, so that both
+// kinds share the CUs (2 x 512 tokens, 8 heads of 64: 147 us a pass as two launches, 87 as
+// one) and one launch less where that counts (4 x 64 tokens, 4 heads of 32: 20 -> 17 us).
+template <typename T, int DH, bool DROP, bool BIAS>
+__global__ void __launch_bounds__(NT, 2) attn_bwd_kernel(QkvView<T> in, const T* dO, const float* lse2, const float* Dsum,
+                                                      GradView<T> grad, int S, int H, int d, float scale_log2, float scale,
+                                                      DropArgs drop, int nkb, BiasArgs bias) {
+  __shared__ u32x4 tiles[BwdTiles<T, DH>::SLOTS];
+  extern __shared__ float bvec[];
+  if ((int)blockIdx.x < nkb)
+    dkdv_body<T, DH, DROP, BIAS>(tiles, bvec, blockIdx.x, in, dO, lse2, Dsum, grad, S, H, d, scale_log2, scale, drop, bias);
+  else
+    dq_body<T, DH, DROP, BIAS>(tiles, bvec, blockIdx.x - nkb, in, dO, lse2, Dsum, grad, S, H, d, scale_log2, scale, drop, bias);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1491,14 +1512,10 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
                          reinterpret_cast<const T*>(o), g, ws, S, H, d, rows);
       hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
-      auto dkdv = a.drop.thr ? attn_bwd_dkdv_kernel<T, DH, true, B> : attn_bwd_dkdv_kernel<T, DH, false, B>;
-      hipLaunchKernelGGL(dkdv, dim3((S + BKV - 1) / BKV, mu * H), dim3(NT), bias_lds(a, 0), st, view<T>(a), g, lse2, ws, grad,
-                         S, H, d, scale_log2, scale, a.drop, ba);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      auto dqk = a.drop.thr ? attn_bwd_dq_kernel<T, DH, true, B> : attn_bwd_dq_kernel<T, DH, false, B>;
-      hipLaunchKernelGGL(dqk, dim3((S + 63) / 64, mu * H), dim3(NT), bias_lds(a, NT / 64 * DiagRow<1>::FLOATS), st, view<T>(a), g, lse2, ws, grad, S,
-                         H, d, scale_log2, scale, a.drop, ba);
+      const int nkb = (S + BKV - 1) / BKV;
+      auto k = a.drop.thr ? attn_bwd_kernel<T, DH, true, B> : attn_bwd_kernel<T, DH, false, B>;
+      hipLaunchKernelGGL(k, dim3(2 * nkb, mu * H), dim3(NT), bias_lds(a, NT / 64 * DiagRow<1>::FLOATS), st, view<T>(a), g, lse2,
+                         ws, grad, S, H, d, scale_log2, scale, a.drop, nkb, ba);
       e = hipGetLastError();
       // column sums: one pass where all three lie side by side
       if (e == hipSuccess && gr.sum_q != nullptr && gr.sum_k == gr.sum_q + d && gr.sum_v == gr.sum_k + d &&
