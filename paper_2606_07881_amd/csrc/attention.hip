@@ -13,8 +13,8 @@
 // transposed in that same order. The saved statistic is
 // lse2 = max + log2(sum), in log2 units of the scaled scores.
 //
-// Backward: D = rowsum(dO * O) first. Then two kernels recompute P from
-// q, k and lse2, so neither needs atomics:
+// Backward: D = rowsum(dO * O) first. Then two kinds of workgroup, in one launch,
+// recompute P from q, k and lse2, so neither needs atomics:
 //   dK/dV  (per 64 keys; 16 keys per wavefront):  S = Q K^T and dP = dO V^T
 //          with the key in the lane, dV^T += dO^T P, dK^T += Q^T dS;
 //   dQ     (per 64 queries; 16 per wavefront):   S^T and dP^T with the query

@@ -23,6 +23,8 @@ CASES = {
     "rope_ragged_bf16": ("ragged_bf16", dict(ROPE, rope_dims=64)),
     "rel_ragged_bf16": ("ragged_bf16", REL),
     "all_ragged_bf16": ("ragged_bf16", ALL),
+    # a table of 24 elements: the tensors behind it begin 16 bytes off a 32-byte boundary
+    "rel8_ragged_bf16": ("ragged_bf16", dict(ALL, rel_buckets=8, rel_max_distance=100)),
     "all_dh128_bf16": ("dh128_bf16", dict(ALL, rope_dims=128, rope_pairs="adjacent")),
     "all_dh32_bf16": ("dh32_bf16", ALL),
     "all_ckpt_ragged_bf16": ("ckpt_ragged_bf16", ALL),
