@@ -360,7 +360,8 @@ int paci_qk_norm_rope_forward(const paci_qk_shapes* s, const void* dev_x, int64_
  * positions and frequencies. dev_g_q_gain / dev_g_k_gain ([head_dim] fp32,
  * nullable; NULL without norm) += the gains' gradients; dev_g_bias
  * ([(q_heads + k_heads) * head_dim] fp32, nullable) += the column sums of
- * dL/dx, the bias gradient of the projection that made x. dev_dx may be dev_dy
+ * dL/dx, the bias gradient of the projection that made x. The three may not
+ * overlap (a gain shared by both kinds: add up two buffers). dev_dx may be dev_dy
  * with the same stride, not dev_x. Without norm, dev_x is not read. dev_ws:
  * paci_qk_norm_rope_workspace bytes, 16-byte aligned (not read without norm
  * and dev_g_bias). Errors as above, and E_NOMEM (workspace too small). */
@@ -377,7 +378,10 @@ int paci_qk_norm_rope_backward(const paci_qk_shapes* s, const void* dev_x, int64
  * bounds[1 .. n_buckets - 1] at or below min(n, max_distance). Table entries at
  * or below -1e9 (-inf, the lowest float) hide their distances from that head;
  * a query with no key left has o = 0 and lse2 = -inf and passes no gradient on.
- * Finite entries above 1e9 count as 1e9.
+ * Finite entries above 1e9 count as 1e9. The operands are finite, in padding
+ * rows too: a hidden or later key has probability zero, and zero times an
+ * infinity or NaN is NaN in a product of matrices, so a non-finite row of k or
+ * v can reach every query of its sequence that shares a block of keys with it.
  * n_buckets = 0: no bias (table, bounds and their gradient NULL). */
 typedef struct paci_attn_shapes {
   int32_t dtype;        /* enum paci_dtype, of q, k, v, o and their gradients */

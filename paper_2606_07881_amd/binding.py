@@ -428,6 +428,7 @@ class Stage:
 # written for few Python operations: a small call costs more here than on the GPU.
 _TORCH_DTYPES = {torch.bfloat16: BF16, torch.float32: FP32}
 _F32, _I32, _F64 = torch.float32, torch.int32, torch.float64
+_INT_MAX = 2 ** 31 - 1   # sizes are int32 in the C structures, which would keep the low bits of larger ones
 
 
 def rope_freqs(theta, rope_dims):
@@ -508,7 +509,7 @@ def _qk_shapes(x, q_heads, k_heads, seq, norm, eps, freq, pairs):
     dt = _operand(x, "qk_norm_rope x")
     tokens, cols = x.shape
     heads = q_heads + k_heads
-    if heads < 1 or cols % heads or pairs not in ROPE_PAIRS:
+    if heads < 1 or min(q_heads, k_heads) < 0 or cols % heads or pairs not in ROPE_PAIRS or max(tokens, cols, seq) > _INT_MAX:
         _refuse(f"qk_norm_rope: {cols} columns of {heads} heads, pairs {pairs!r}")
     return PaciQkShapes(dt, tokens, seq, q_heads, k_heads, cols // heads, norm, eps, 0 if freq is None else 2 * freq.numel(),
                         ROPE_PAIRS[pairs])
@@ -553,7 +554,7 @@ def qk_norm_rope_backward(x, dy, dx, q_heads, k_heads, seq=1, q_gain=None, k_gai
 def _attn_shapes(q, batch, n_heads, table, max_distance):
     dt = _operand(q, "attention q")
     T, d = q.shape
-    if batch < 0 or n_heads < 1 or d % n_heads or (T % batch if batch else T):
+    if batch < 0 or n_heads < 1 or d % n_heads or (T % batch if batch else T) or max(T, d, batch, max_distance) > _INT_MAX:
         _refuse(f"attention: {(T, d)} is not {batch} sequences of {n_heads} heads")
     return PaciAttnShapes(dt, batch, T // batch if batch else 0, n_heads, d // n_heads, 0 if table is None else table.shape[0],
                           max_distance)

@@ -18,6 +18,11 @@ bool rows_ok(const void* p, int64_t ld, int64_t cols, int64_t rows, int dtype) {
   return p && aligned(p, 16) && ld % vec == 0 && (ld >= cols || (rows <= 1 && ld >= 0)) && ld <= (1LL << 46) / rows;
 }
 bool floats_ok(const float* p) { return p && aligned(p, 4); }
+// Whether a[na] and b[nb] share an element (null: no).
+bool overlap(const float* a, int64_t na, const float* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + 4 * (uintptr_t)nb && y < x + 4 * (uintptr_t)na;
+}
 
 int done(hipError_t e) {
   if (e == hipSuccess) return PACI_OK;
@@ -145,6 +150,11 @@ extern "C" int paci_qk_norm_rope_backward(const paci_qk_shapes* s, const void* d
     return PACI_E_INVAL;
   if (!s->norm && (dev_g_q_gain || dev_g_k_gain)) return PACI_E_INVAL;
   if (!aligned(dev_g_q_gain, 4) || !aligned(dev_g_k_gain, 4) || !aligned(dev_g_bias, 4)) return PACI_E_INVAL;
+  // different workgroups add to them at once
+  const int64_t dh = s->head_dim;
+  if (overlap(dev_g_q_gain, dh, dev_g_k_gain, dh) || overlap(dev_g_q_gain, dh, dev_g_bias, cols) ||
+      overlap(dev_g_k_gain, dh, dev_g_bias, cols))
+    return PACI_E_INVAL;
   paci::RotArgs r = rot_args(*s);
   if (s->norm || dev_g_bias) {
     if (!dev_ws || !aligned(dev_ws, 16)) return PACI_E_INVAL;

@@ -207,7 +207,7 @@ ATTN = [
     (1, 1, 1, 32, 8, 16, ""), (2, 2, 3, 64, 32, 128, ""), (1, 17, 2, 64, 8, 5, ""), (3, 63, 1, 32, 16, 40, "far"),
     (2, 64, 2, 64, 32, 128, ""), (1, 65, 3, 64, 2, 2, ""), (2, 100, 2, 32, 16, 33, "first"), (1, 129, 2, 64, 8, 64, "all"),
     (2, 200, 3, 64, 32, 128, "some"), (1, 300, 2, 32, 64, 200, "lowest"), (1, 333, 1, 64, 4, 3, "far"),
-    (1, 700, 1, 64, 32, 512, ""), (1, 520, 2, 32, 8, 100, "big"), (1, 200, 2, 64, 0, 0, ""),
+    (1, 700, 1, 64, 32, 512, ""), (1, 4500, 1, 64, 32, 128, ""), (1, 520, 2, 32, 8, 100, "big"), (1, 200, 2, 64, 0, 0, ""),
 ]
 # enough (sequence, head) pairs for the larger workgroups
 ATTN_MANY = [(8, 260, 16, 64, 32, 128, ""), (3, 250, 47, 32, 16, 30, "some"), (11, 193, 16, 64, 8, 300, "far"),
@@ -373,6 +373,84 @@ def test_attention_with_an_entry_beyond_every_score(binding, dtype, entry):
     g_table = torch.zeros(8, H, device="cuda")
     binding.attention_backward(q, k, v, o, lse2, dev(c.do, dtype), *grads, g_table=g_table, **kw)
     assert all(torch.isfinite(t).all() for t in grads + [g_table])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_offsets_beyond_32_bits(binding, dtype):
+    """Rows of one sequence further apart than 2^31 elements: the bits of the same call on dense copies."""
+    import torch
+    B, S, dh, ld = 2, 20000, 64, 131072
+    T, act = B * S, torch.bfloat16 if dtype == "bf16" else torch.float32
+    torch.manual_seed(4)
+    wide, out = (torch.empty(T, ld, device="cuda", dtype=act) for _ in range(2))
+    dense = torch.randn(T, 3 * dh, device="cuda").to(act)
+    # the third columns end a row, so the last row's end is the buffer's
+    cols = [slice(0, dh), slice(4096, 4096 + dh), slice(ld - dh, ld)]
+    for i, c in enumerate(cols):
+        wide[:, c] = dense[:, i * dh:(i + 1) * dh]
+    gain, do = torch.rand(dh, device="cuda") + 0.5, torch.randn(T, dh, device="cuda").to(act)
+    freq = torch.from_numpy(binding.rope_freqs(1e4, dh)).cuda()
+    table, bounds = torch.randn(32, 1, device="cuda"), torch.from_numpy(binding.rel_bounds(32, 128)).cuda()
+    rot = dict(q_heads=1, k_heads=0, seq=S, q_gain=gain, freq=freq)
+    rel = dict(batch=B, n_heads=1, table=table, bounds=bounds, max_distance=128)
+
+    def chain(x, y, g):
+        """x: three columns of inputs, y: of results (the rotation and its backward in the last)."""
+        o, lse2 = torch.empty(T, dh, device="cuda", dtype=act), torch.empty(B, S, device="cuda")
+        binding.attention(*x, o, lse2, **rel)
+        binding.attention_backward(*x, o, lse2, do, *y, g_table=g[0], **rel)
+        grads = [t.clone() for t in y]
+        binding.qk_norm_rope(x[2], y[2], **rot)
+        turned = y[2].clone()
+        binding.qk_norm_rope_backward(x[2], y[2], y[2], g_q_gain=g[1], g_bias=g[2], **rot)
+        return [o, lse2, *grads, turned, y[2].clone(), *g]
+
+    def zeros():
+        return [torch.zeros(32, 1, device="cuda"), torch.zeros(dh, device="cuda"), torch.zeros(dh, device="cuda")]
+    near = chain(list(dense.split(dh, 1)), [torch.empty(T, dh, device="cuda", dtype=act) for _ in range(3)], zeros())
+    far = chain([wide[:, c] for c in cols], [out[:, c] for c in cols], zeros())
+    for i, (a, b) in enumerate(zip(near, far)):
+        assert torch.isfinite(a).all() and torch.equal(a, b), i
+
+
+def test_calls_at_once_on_two_streams(binding):
+    """Two chains of different sizes enqueued side by side, workspaces from the allocator: the bits of each alone."""
+    import torch
+    torch.manual_seed(9)
+
+    def make(B, S, H, dh, act):
+        d, T = H * dh, B * S
+        x, do = torch.randn(T, 3 * d, device="cuda").to(act), torch.randn(T, d, device="cuda").to(act)
+        gain, table = torch.rand(dh, device="cuda") + 0.5, torch.randn(16, H, device="cuda")
+        freq, bounds = torch.from_numpy(binding.rope_freqs(1e4, dh)).cuda(), torch.from_numpy(binding.rel_bounds(16, 50)).cuda()
+        rot = dict(q_heads=H, k_heads=H, seq=S, q_gain=gain, k_gain=gain, freq=freq)
+        rel = dict(batch=B, n_heads=H, table=table, bounds=bounds, max_distance=50)
+
+        def chain():
+            qk, o, lse2 = torch.empty(T, 2 * d, device="cuda", dtype=act), torch.empty_like(do), torch.empty(B * H, S, device="cuda")
+            dqkv, g = torch.empty_like(x), torch.zeros(2 * dh + 16 * H, device="cuda")
+            gq, gk, gt = g.split([dh, dh, 16 * H])
+            binding.qk_norm_rope(x[:, :2 * d], qk, **rot)
+            q, k = qk.split(d, 1)
+            binding.attention(q, k, x[:, 2 * d:], o, lse2, **rel)
+            binding.attention_backward(q, k, x[:, 2 * d:], o, lse2, do, *dqkv.split(d, 1), g_table=gt.view(16, H), **rel)
+            binding.qk_norm_rope_backward(x[:, :2 * d], dqkv[:, :2 * d], dqkv[:, :2 * d], g_q_gain=gq, g_k_gain=gk, **rot)
+            return o, lse2, dqkv, g
+        return chain
+    chains = [make(4, 300, 8, 64, torch.bfloat16), make(2, 190, 4, 32, torch.float32)]
+    alone = [c() for c in chains]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in chains]
+    got = [[], []]
+    for _ in range(4):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(chains[i]())
+    torch.cuda.synchronize()
+    for i, runs in enumerate(got):
+        for r in runs:
+            for a, b in zip(alone[i], r):
+                assert torch.equal(a, b), i
 
 
 def test_first_call_of_a_process_can_be_captured(binding, root):

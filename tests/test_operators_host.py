@@ -53,8 +53,8 @@ def qk_fwd(s, **over):
 
 
 def qk_bwd(s, **over):
-    p = dict(x=A, ldx=256, dy=3 * A, lddy=256, gq=A, gk=A, pos=None, freq=A, dx=2 * A, lddx=256, wq=A, wk=A, wb=A, ws=A,
-             n=1 << 40)
+    p = dict(x=A, ldx=256, dy=3 * A, lddy=256, gq=A, gk=A, pos=None, freq=A, dx=2 * A, lddx=256, wq=A, wk=A + 256,
+             wb=A + 512, ws=A, n=1 << 40)
     p.update(over)
     return lib.paci_qk_norm_rope_backward(ctypes.byref(s), p["x"], p["ldx"], p["dy"], p["lddy"], p["gq"], p["gk"], p["pos"],
                                           p["freq"], p["dx"], p["lddx"], p["wq"], p["wk"], p["wb"], p["ws"], p["n"], None)
@@ -78,6 +78,10 @@ def test_qk_buffers_are_refused():
         assert qk_fwd(s, **over) == INVAL, over
     for over in [dict(dy=None), dict(dy=3 * A + 8), dict(lddy=128), dict(dx=None), dict(dx=2 * A + 8), dict(lddx=128),
                  dict(dx=3 * A, lddx=264), dict(dx=A), dict(wq=A + 2), dict(wb=A + 1), dict(ws=None), dict(ws=A + 4)]:
+        assert qk_bwd(s, **over) == INVAL, over
+    # parameter gradients that share elements: 64 of a gain each, 256 column sums
+    for over in [dict(wk=A), dict(wk=A + 252), dict(wk=A - 252), dict(wb=A), dict(wb=A + 256), dict(wb=A + 508),
+                 dict(wb=A - 1020), dict(wq=None, wb=A + 256)]:
         assert qk_bwd(s, **over) == INVAL, over
     n = ctypes.c_size_t(0)
     assert lib.paci_qk_norm_rope_workspace(ctypes.byref(s), ctypes.byref(n)) == 0 and n.value > 0
@@ -153,6 +157,32 @@ def test_binding_refuses_what_it_cannot_pass_on():
         with pytest.raises(binding.PaciError) as e:
             call()
         assert e.value.code == INVAL   # host tensors
+
+
+class Shape:
+    """A matrix on a device as far as sizes go."""
+    is_cuda, dtype = True, torch.bfloat16
+
+    def __init__(self, *shape):
+        self.shape = shape
+
+    def dim(self):
+        return len(self.shape)
+
+
+def test_binding_refuses_sizes_beyond_the_c_types():
+    """Sizes are 32-bit in the C structures: one that does not fit is refused, not cut to its low bits."""
+    big = 2 ** 32
+    for call in (lambda: binding.qk_norm_rope_workspace(Shape(big + 4, 128), 1, 1),
+                 lambda: binding.qk_norm_rope_workspace(Shape(4, 128), 1, 1, seq=big + 4),
+                 lambda: binding.qk_norm_rope_workspace(Shape(4, 128), big + 2, -big),
+                 lambda: binding.attention_workspace(Shape(big + 4, 128), 1, 2),
+                 lambda: binding.attention_workspace(Shape(big + 4, 128), big + 4, 2),
+                 lambda: binding.attention_workspace(Shape(4, 128), 1, 2, table=torch.zeros(8, 2), max_distance=big + 32)):
+        with pytest.raises(binding.PaciError):
+            call()
+    assert binding.qk_norm_rope_workspace(Shape(4, 128), 1, 1, seq=4) > 0
+    assert binding.attention_workspace(Shape(4, 128), 1, 2, table=torch.zeros(8, 2), max_distance=32) > 0
 
 
 # ---- the same as options of a stage -------------------------------------------------------
