@@ -38,7 +38,7 @@ namespace paci {
 namespace {
 
 constexpr int NT = 256;       // threads of a workgroup that takes whole tokens
-constexpr int NT_MAX = 512;   // of one that takes a part of a token's heads
+constexpr int NT_MAX = 512;   // of one that takes a part of a token's heads, or wide tokens in the backward
 
 struct RotKernelArgs {
   const void* x; int64_t ldx;
@@ -331,7 +331,13 @@ __global__ void __launch_bounds__(NT) rotary_sums_kernel(const float* __restrict
 // forward (4 in bf16, 2 in fp32), half that in the backward, which reads two rows and
 // holds its sums (8192 tokens, 16 + 16 heads of 64, bf16: 30.5 us with 2, 43 with 4
 // in 256 registers and spills to the second file, 30.7 with 1). Backward workgroups
-// each leave a row of sums, so there are two to a CU (30.5; one 33.8, three 38.5).
+// each leave a row of sums, so there are few: two of 256 threads to a CU (30.5; one
+// 33.8, three 38.5), or, where a token has more than 128 lanes and 256 threads would
+// hold one or two, one of up to 512. bf16 and fp32, us with two of 256 / one of 512:
+// 8192 tokens of 16 + 16 heads of 128: 48.2 / 45.7, 89.9 / 86.6; 32768 of 32 + 8 heads of
+// 128: 238 / 225; 4096 of 32 + 8 in fp32: 64.7 / 55.8; 4096 of 16 + 4 heads of 128:
+// 28.2 / 25.2; but 16 + 16 heads of 64: 30.4 / 30.2, 42.6 / 43.0, 12 + 12: 27.4 / 28.5
+// and 32768 tokens of 1 + 1: 17.1 / 19.2.
 struct RotPlan {
   int lpr, slots, part, par, U, chunks, threads, gx, gy;
   size_t lds;
@@ -342,11 +348,13 @@ RotPlan rot_plan(const RotArgs& r, bool bwd) {
   for (p.lpr = 1; 16 * p.lpr < r.dh;) p.lpr *= 2;
   const int rows = r.q_heads + r.k_heads;
   p.slots = rows * p.lpr;
+  const bool wide = bwd && p.slots > NT / 2;
+  const int nt = wide ? NT_MAX : NT, per_cu = wide ? 1 : 2;
   // a token's heads in as few workgroups as hold them, evenly; several tokens side by side if they are few
-  p.gy = p.slots <= NT ? 1 : (p.slots + NT_MAX - 1) / NT_MAX;
+  p.gy = p.slots <= nt ? 1 : (p.slots + NT_MAX - 1) / NT_MAX;
   p.part = (rows + p.gy - 1) / p.gy * p.lpr;
   p.gy = (p.slots + p.part - 1) / p.part;
-  p.par = std::max(1, NT / p.part);
+  p.par = std::max(1, nt / p.part);
   p.U = (r.dt == DT_BF16 ? 4 : 2) / (bwd ? 2 : 1);
   // the backward walks chunks with two buffers of angles, the forward takes one chunk per workgroup
   const size_t token = (size_t)(bwd ? 2 : 1) * (r.rope_dims / 2) * sizeof(float2);   // LDS per token
@@ -356,7 +364,7 @@ RotPlan rot_plan(const RotArgs& r, bool bwd) {
   if ((int64_t)((r.T + p.U * p.par - 1) / (p.U * p.par)) * p.gy < cu_count()) p.U = 1;
   p.chunks = (r.T + p.U * p.par - 1) / (p.U * p.par);
   p.gx = p.chunks;
-  if (bwd) p.gx = std::min(p.chunks, std::max(1, 2 * cu_count() / p.gy));
+  if (bwd) p.gx = std::min(p.chunks, std::max(1, per_cu * cu_count() / p.gy));
   p.threads = (p.par * p.part + 63) / 64 * 64;
   p.lds = token * p.U * p.par;
   if (bwd) p.lds = std::max(p.lds, (size_t)p.threads * 16 * sizeof(float));   // the sums at its end

@@ -69,7 +69,7 @@ ROTARY = [
     (200, 7, 7, 128, 48, "half", True, "seq"), (65, 17, 2, 256, 256, "half", True, "seq"),
     (66, 9, 9, 256, 64, "adjacent", True, "given"), (300, 2, 1, 80, 0, "half", True, "seq"),
     (700, 1, 1, 16, 16, "adjacent", True, "seq"), (90, 40, 8, 112, 112, "half", True, "given"),
-    (2100, 16, 16, 64, 64, "half", True, "seq"), (1025, 12, 12, 64, 64, "half", False, "far"),
+    (2100, 16, 16, 64, 64, "half", True, "seq"), (2100, 16, 4, 128, 128, "half", True, "seq"), (1025, 12, 12, 64, 64, "half", False, "far"),
     (70, 80, 17, 128, 128, "half", True, "seq"), (33, 75, 75, 256, 128, "adjacent", True, "given"),
 ]
 
