@@ -19,7 +19,7 @@
 // dx stay in registers. The tokens of a workgroup are taken U to a thread at a
 // time: their loads are issued first, then the workgroup computes the angles of
 // those tokens once for all heads, into LDS. Measured (kernel): 8192 tokens of 16 + 16
-// heads of 64, bf16: forward 14.4 us, 4.7 TB/s; backward 26 us, 3.9 TB/s, and 4.5 us
+// heads of 64, bf16: forward 14.4 us, 4.7 TB/s; backward 24 us, 4.2 TB/s, and 4 us
 // for the sums' second launch (a 1 GiB copy reaches 5.1 TB/s on this card).
 //
 // Angles: pos * freq in 64 bits and reduced to a fraction of a turn there (a 32-bit
@@ -116,7 +116,7 @@ template <int SIGN> __device__ __forceinline__ void rotate(float (&f)[16], const
 // U: tokens of a thread in flight.
 template <typename T, int LPR, int U, bool NORM, bool BWD>
 __global__ void __launch_bounds__(NT_MAX) rotary_kernel(RotKernelArgs a) {
-  extern __shared__ floatx4 lds[];   // angles [U * par][R / 2] (cos, sin), two buffers in the backward; then its sums, 16 floats a thread
+  extern __shared__ floatx4 lds[];   // angles [U * par][R / 2] (cos, sin), two buffers in the backward; then its sums, 32 floats a thread
   const int tid = threadIdx.x, nt = blockDim.x;
   const int R2 = a.R / 2;
   const int p = tid / a.part;                                   // the thread's token within the workgroup
@@ -248,54 +248,68 @@ __global__ void __launch_bounds__(NT_MAX) rotary_kernel(RotKernelArgs a) {
     }
   }
   if constexpr (BWD) {
-    // column sums of the workgroup: over its tokens side by side (bias), and over the heads too (gains)
-    float* red = reinterpret_cast<float*>(lds);   // [thread][16], 4-float units rotated by the thread (17-float rows would break 16-byte stores)
-    auto put = [&](const float (&v)[16]) {
+    // Sums of the workgroup, in halving rounds: the upper half of the members leaves its sums in
+    // LDS, the lower half adds them (a round's writers are none of the round before's readers'
+    // sources, so one barrier a round). First the tokens side by side; then the column sums are
+    // whole, and the gains' add up over the heads of their kind.
+    floatx4* red = lds;   // [thread][4] of sb, then of sg; units rotated by the thread against bank conflicts
+    auto put = [&](const float (&v)[16], int part) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        reinterpret_cast<floatx4*>(red)[tid * 4 + ((q + (tid >> 1)) & 3)] = floatx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        red[(part * nt + tid) * 4 + ((q + (tid >> 1)) & 3)] = floatx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
     };
-    auto get = [&](int th, int j) { return red[th * 16 + 4 * (((j >> 2) + (th >> 1)) & 3) + (j & 3)]; };
-    // thread (within a token's slots) and element that hold element e of a row
-    auto where = [&](int e, int& lane, int& j) {
-      if (a.adjacent) {
-        lane = e >> 4;
-        j = e & 15;
-      } else {
-        const int base = e < a.R ? 0 : a.R, half = (e < a.R ? a.R : a.dh - a.R) / 2, q = e - base;
-        const int s = q >= half;
-        lane = base / 16 + ((q - s * half) >> 3);
-        j = 8 * s + ((q - s * half) & 7);
+    auto add = [&](float (&v)[16], int part, int from) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const floatx4 u = red[(part * nt + from) * 4 + ((q + (from >> 1)) & 3)];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[4 * q + r] += u[r];
       }
     };
-    const int row0 = blockIdx.y * a.part / LPR;                        // first row of this workgroup
-    const int rows = min(a.part, a.slots - (int)blockIdx.y * a.part) / LPR;
-    if (a.part_bias != nullptr) {
-      __syncthreads();
-      put(sb);
-      __syncthreads();
-      for (int k = tid; k < rows * a.dh; k += nt) {
-        const int r = k / a.dh, e = k - r * a.dh;
-        int lane, j;
-        where(e, lane, j);
-        float s = 0.f;
-        for (int q = 0; q < a.par; ++q) s += get(q * a.part + r * LPR + lane, j);
-        a.part_bias[(int64_t)blockIdx.x * (a.Hq + a.Hk) * a.dh + (int64_t)(row0 + r) * a.dh + e] = s;
+    auto out16 = [&](float* to, const float (&v)[16]) {   // the thread's columns of a row
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<floatx4*>(to + (q < 2 ? oa : ob) + 4 * (q & 1)) =
+            floatx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    };
+    const bool bias = a.part_bias != nullptr;
+    if (NORM || bias) {
+      __syncthreads();   // the angles' last readers
+      for (int n = a.par, half; n > 1; n = half) {
+        half = (n + 1) / 2;
+        if (p >= half && p < n) {
+          if (bias) put(sb, 0);
+          if (NORM) put(sg, 1);
+        }
+        __syncthreads();
+        if (p < n - half) {
+          if (bias) add(sb, 0, tid + half * a.part);
+          if (NORM) add(sg, 1, tid + half * a.part);
+        }
       }
     }
+    if (bias && live && p == 0) out16(a.part_bias + ((int64_t)blockIdx.x * (a.Hq + a.Hk) + row) * a.dh, sb);
     if constexpr (NORM) {
-      __syncthreads();
-      put(sg);
-      __syncthreads();
-      for (int k = tid; k < 2 * a.dh; k += nt) {
-        const bool key = k >= a.dh;
-        int lane, j;
-        where(key ? k - a.dh : k, lane, j);
-        const int ra = key ? max(a.Hq - row0, 0) : 0, rb = key ? rows : min(rows, a.Hq - row0);
-        float s = 0.f;
-        for (int q = 0; q < a.par; ++q)
-          for (int r = ra; r < rb; ++r) s += get(q * a.part + r * LPR + lane, j);
-        a.part_gain[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.dh + k] = s;
+      const int row0 = blockIdx.y * a.part / LPR;                        // first row of this workgroup
+      const int rows = min(a.part, a.slots - (int)blockIdx.y * a.part) / LPR;
+      const int nq = min(max(a.Hq - row0, 0), rows), nk = rows - nq;
+      const bool key = row >= a.Hq;
+      const int idx = row - row0 - (key ? nq : 0), len = key ? nk : nq;   // among the rows of its kind
+      for (int n = max(nq, nk), half; n > 1; n = half) {
+        half = (n + 1) / 2;
+        const int end = p == 0 ? min(n, len) : 0;
+        if (idx >= half && idx < end) put(sg, 1);
+        __syncthreads();
+        if (idx + half < end) add(sg, 1, tid + half * LPR);
+      }
+      if (live && p == 0 && idx == 0) {
+        float* to = a.part_gain + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.dh;
+        out16(to + (key ? a.dh : 0), sg);
+        if (len == rows) {   // no head of the other kind here
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sg[j] = 0.f;
+          out16(to + (key ? 0 : a.dh), sg);
+        }
       }
     }
   }
@@ -329,15 +343,14 @@ __global__ void __launch_bounds__(NT) rotary_sums_kernel(const float* __restrict
 
 // The launch of a pass. U tokens in flight per thread: 64 bytes a vector pair in the
 // forward (4 in bf16, 2 in fp32), half that in the backward, which reads two rows and
-// holds its sums (8192 tokens, 16 + 16 heads of 64, bf16: 30.5 us with 2, 43 with 4
-// in 256 registers and spills to the second file, 30.7 with 1). Backward workgroups
-// each leave a row of sums, so there are few: two of 256 threads to a CU (30.5; one
-// 33.8, three 38.5), or, where a token has more than 128 lanes and 256 threads would
-// hold one or two, one of up to 512. bf16 and fp32, us with two of 256 / one of 512:
-// 8192 tokens of 16 + 16 heads of 128: 48.2 / 45.7, 89.9 / 86.6; 32768 of 32 + 8 heads of
-// 128: 238 / 225; 4096 of 32 + 8 in fp32: 64.7 / 55.8; 4096 of 16 + 4 heads of 128:
-// 28.2 / 25.2; but 16 + 16 heads of 64: 30.4 / 30.2, 42.6 / 43.0, 12 + 12: 27.4 / 28.5
-// and 32768 tokens of 1 + 1: 17.1 / 19.2.
+// holds its sums (with 4 it takes 256 registers and spills to the second file: 13 us more
+// at 8192 tokens of 16 + 16 heads of 64 in bf16; 1 is as fast there). Backward workgroups
+// each leave a row of sums, so there are few: two of 256 threads to a CU (27.4 us there;
+// one 30.6, three 32.4), or one of up to 512 where a token has 128 lanes or more. us with
+// two of 256 / one of 512: 8192 tokens of 16 + 16 heads of 64: 27.4 / 26.7, in fp32 39.6 /
+// 39.6; of 128: 43.7 / 42.8, 86.4 / 84.4; 32768 of 32 + 8 heads of 128: 227 / 219; 4096 of
+// 32 + 8 in fp32: 56.1 / 50.7; but 12 + 12 heads of 64: 24.4 / 25.5, 16384 tokens of 8 + 2
+// heads of 96: 30.8 / 31.2.
 struct RotPlan {
   int lpr, slots, part, par, U, chunks, threads, gx, gy;
   size_t lds;
@@ -348,7 +361,7 @@ RotPlan rot_plan(const RotArgs& r, bool bwd) {
   for (p.lpr = 1; 16 * p.lpr < r.dh;) p.lpr *= 2;
   const int rows = r.q_heads + r.k_heads;
   p.slots = rows * p.lpr;
-  const bool wide = bwd && p.slots > NT / 2;
+  const bool wide = bwd && p.slots >= NT / 2;
   const int nt = wide ? NT_MAX : NT, per_cu = wide ? 1 : 2;
   // a token's heads in as few workgroups as hold them, evenly; several tokens side by side if they are few
   p.gy = p.slots <= nt ? 1 : (p.slots + NT_MAX - 1) / NT_MAX;
@@ -367,7 +380,7 @@ RotPlan rot_plan(const RotArgs& r, bool bwd) {
   if (bwd) p.gx = std::min(p.chunks, std::max(1, per_cu * cu_count() / p.gy));
   p.threads = (p.par * p.part + 63) / 64 * 64;
   p.lds = token * p.U * p.par;
-  if (bwd) p.lds = std::max(p.lds, (size_t)p.threads * 16 * sizeof(float));   // the sums at its end
+  if (bwd) p.lds = std::max(p.lds, (size_t)p.threads * 32 * sizeof(float));   // the sums at its end
   return p;
 }
 
