@@ -1361,30 +1361,37 @@ __global__ void __launch_bounds__((BwdRing<DH, SMALL>::NTB), (BwdRing<DH, SMALL>
 // g_table[b][h] += the sum over sequences, wavefronts (wr queries each, `rows` of them) and
 // the distances of bucket b of part [head][sequence][wavefront][max_distance + 1]. A
 // wavefront has entries for the distances its queries reach. A workgroup takes the buckets
-// of a head that begin at one of 32 distances (32 blockIdx.x and on): it sums their
+// of a head that begin at one of 16 distances (16 blockIdx.y and on): it sums their
 // distances over the rows, side by side, then a wavefront adds up a bucket. All in a fixed
-// order. (A workgroup per bucket reads narrow columns, which every XCD fetches again: 17 us
-// for 4 x 128 rows of 257 and 16 heads.)
-constexpr int BS_NT = 512, BS_SPAN = 32;
+// order. Latency-bound: 16 loads a thread in flight, one round of them up to 512 rows. The
+// columns are narrower than a cache line, so the workgroups of a head follow each other H
+// apart: with 8 or 16 heads on one XCD, whose L2 then fetches a line once. 256 rows of 129 and
+// 16 heads: 5.9 us (32 distances a workgroup 8.3; the workgroups of a head side by side
+// 6.4), 512 rows of 257: 7.8 (11.0, 10.1), 512 of 513: 12.6 (11.5, 15.7).
+constexpr int BS_NT = 512, BS_SPAN = 16;
 __global__ void __launch_bounds__(BS_NT) attn_bias_sums_kernel(const float* __restrict__ part, int batch, int rows, int wr, int H,
                                                                const int32_t* __restrict__ bounds, int n_buckets,
                                                                int max_distance, float* g_table) {
   __shared__ float red[BS_NT];
   __shared__ float dist[MAX_DISTANCE + 1];
-  __shared__ int begin[MAX_BUCKETS + 1];   // first distance of every bucket, and the end
-  const int h = blockIdx.y, n = max_distance + 1, c = threadIdx.x & 63, rg = threadIdx.x >> 6;
-  for (int b = threadIdx.x; b <= n_buckets; b += BS_NT)
-    begin[b] = b == 0 ? 0 : b < n_buckets ? min(max(bounds[b], 0), n) : n;
-  __syncthreads();
-  int b0 = 0, b1 = 0;   // the workgroup's buckets
-  for (int b = c; b < n_buckets; b += 64) {   // every wavefront counts for itself
-    b0 += begin[b] < BS_SPAN * (int)blockIdx.x;
-    b1 += begin[b] < BS_SPAN * ((int)blockIdx.x + 1);
+  __shared__ int begin[MAX_BUCKETS + 1];   // first distance of every bucket, then the end
+  const int h = blockIdx.x, n = max_distance + 1, c = threadIdx.x & 63, rg = threadIdx.x >> 6;
+  const int total = batch * rows;
+  int b0 = 0, b1 = 0;   // the workgroup's buckets; every wavefront counts for itself
+#pragma unroll
+  for (int k = 0; k < MAX_BUCKETS / 64; ++k) {
+    const int b = 64 * k + c;
+    const int v = b == 0 ? 0 : b < n_buckets ? min(max(bounds[b], 0), n) : n;
+    if (rg == 0) begin[b] = v;
+    b0 += __popcll(__ballot(b < n_buckets && v < BS_SPAN * (int)blockIdx.y));
+    b1 += __popcll(__ballot(b < n_buckets && v < BS_SPAN * ((int)blockIdx.y + 1)));
   }
-  b0 = (int)wave_sum((float)b0);
-  b1 = (int)wave_sum((float)b1);
+  if (threadIdx.x == 0) begin[MAX_BUCKETS] = n;
   if (b0 >= b1) return;   // uniform
-  const int first = begin[b0], last = begin[b1], total = batch * rows;
+  float* g = g_table + (int64_t)(b0 + rg) * H + h;
+  const float old = b0 + rg < b1 ? *g : 0.f;   // of the wavefront's first bucket
+  __syncthreads();
+  const int first = begin[b0], last = begin[b1];
   int cw = BS_SPAN;   // distances side by side: all of them if they are at most 128
   while (cw < last - first && cw < 128) cw *= 2;
   const int cc = threadIdx.x & (cw - 1), r0 = threadIdx.x / cw, step = BS_NT / cw;
@@ -1405,10 +1412,15 @@ __global__ void __launch_bounds__(BS_NT) attn_bias_sums_kernel(const float* __re
         if (w >= rows) w -= rows;
       }
     }
+    if (cw <= 32) s += __shfl_xor(s, 32, 64);
+    if (cw == 16) s += __shfl_xor(s, 16, 64);
     red[threadIdx.x] = s;
     __syncthreads();
-    if (r0 == 0 && d0 + cc < n) {
-      for (int q = 1; q < step; ++q) s += red[q * cw + cc];
+    if (r0 == 0 && d0 + cc < n) {   // 8 row groups of 64 entries, or 4 of 128
+      const int gs = max(cw, 64);
+      s = 0.f;
+#pragma unroll
+      for (int q = 0; q < BS_NT / 64; ++q) s += q * gs < BS_NT ? red[(q * gs + cc) & (BS_NT - 1)] : 0.f;
       dist[d0 + cc] = s;
     }
     __syncthreads();
@@ -1417,7 +1429,7 @@ __global__ void __launch_bounds__(BS_NT) attn_bias_sums_kernel(const float* __re
     float s = 0.f;
     for (int i = begin[b] + c; i < begin[b + 1]; i += 64) s += dist[i];
     s = wave_sum(s);
-    if (c == 0) g_table[(int64_t)b * H + h] += s;
+    if (c == 0) g_table[(int64_t)b * H + h] = s + (b == b0 + rg ? old : g_table[(int64_t)b * H + h]);
   }
 }
 
@@ -1530,7 +1542,7 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
   hipError_t e = a.table ? launch(std::true_type{}) : launch(std::false_type{});
   if (e != hipSuccess || ba.part == nullptr) return e;
   const int wr = dq_wave_rows(a);
-  hipLaunchKernelGGL(attn_bias_sums_kernel, dim3(a.max_distance / BS_SPAN + 1, H), dim3(BS_NT), 0, st, ba.part, mu, (S + wr - 1) / wr, wr, H,
+  hipLaunchKernelGGL(attn_bias_sums_kernel, dim3(H, a.max_distance / BS_SPAN + 1), dim3(BS_NT), 0, st, ba.part, mu, (S + wr - 1) / wr, wr, H,
                      a.bounds, a.n_buckets, a.max_distance, gr.g_table);
   return hipGetLastError();
 }
