@@ -428,6 +428,8 @@ class Stage:
 # written for few Python operations: a small call costs more here than on the GPU.
 _TORCH_DTYPES = {torch.bfloat16: BF16, torch.float32: FP32}
 _F32, _I32, _F64 = torch.float32, torch.int32, torch.float64
+# the current stream's handle; torch.cuda.current_stream makes a Stream object around it (1 us of a 9 us call)
+_raw_stream = torch._C._cuda_getCurrentRawStream
 _INT_MAX = 2 ** 31 - 1   # sizes are int32 in the C structures, which would keep the low bits of larger ones
 
 
@@ -451,19 +453,19 @@ def _refuse(what, code=E_INVAL):
     raise PaciError(code, what)
 
 
-def _mat(t, shape, like, what):
-    """Address of a matrix of this shape and of like's dtype and device (its stride is the caller's to pass)."""
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device or (t.stride(1) != 1 and shape[1] > 1):
-        _refuse(f"{what}: {tuple(shape)} {like.dtype} on {like.device} with contiguous rows expected")
+def _mat(t, shape, dtype, dev, what):
+    """Address of a matrix of this shape, dtype and device index (its stride is the caller's to pass)."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or (t.stride(1) != 1 and shape[1] > 1):
+        _refuse(f"{what}: {tuple(shape)} {dtype} on device {dev} with contiguous rows expected")
     return t.data_ptr()
 
 
-def _vec(t, shape, dtype, like, what):
+def _vec(t, shape, dtype, dev, what):
     """Address of a contiguous tensor of this shape (None: null)."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous():
-        _refuse(f"{what}: contiguous {shape} {dtype} on {like.device} expected")
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+        _refuse(f"{what}: contiguous {tuple(shape)} {dtype} on device {dev} expected")
     return t.data_ptr()
 
 
@@ -475,10 +477,9 @@ def _operand(x, what):
     return _refuse(what, E_UNSUPPORTED) if dt is None else dt
 
 
-def _launch(fn, like, *args):
-    """Calls a C operator on like's device and current stream."""
-    dev = like.get_device()
-    st = torch.cuda.current_stream(dev).cuda_stream
+def _launch(fn, dev, *args):
+    """Calls a C operator on a device's current stream."""
+    st = _raw_stream(dev)
     if dev == torch.cuda.current_device():
         r = fn(*args, st)
     else:
@@ -521,11 +522,11 @@ def qk_norm_rope(x, y, q_heads, k_heads, seq=1, q_gain=None, k_gain=None, eps=1e
     no norm. freq ([rope_dims / 2] float64): rotation, None: none. pos ([tokens] int32)
     or, without it, row % seq. y may be x."""
     s = _qk_shapes(x, q_heads, k_heads, seq, q_gain is not None or k_gain is not None, eps, freq, pairs)
-    dh = (s.head_dim,)
-    _launch(lib.paci_qk_norm_rope_forward, x, ctypes.byref(s), _mat(x, x.shape, x, "qk_norm_rope x"), x.stride(0),
-            _vec(q_gain, dh, _F32, x, "q_gain"), _vec(k_gain, dh, _F32, x, "k_gain"),
-            _vec(pos, (s.tokens,), _I32, x, "pos"), _vec(freq, (s.rope_dims // 2,), _F64, x, "freq"),
-            _mat(y, x.shape, x, "qk_norm_rope y"), y.stride(0))
+    dh, shape, dt, dev = (s.head_dim,), x.shape, x.dtype, x.get_device()
+    _launch(lib.paci_qk_norm_rope_forward, dev, ctypes.byref(s), _mat(x, shape, dt, dev, "qk_norm_rope x"), x.stride(0),
+            _vec(q_gain, dh, _F32, dev, "q_gain"), _vec(k_gain, dh, _F32, dev, "k_gain"),
+            _vec(pos, (s.tokens,), _I32, dev, "pos"), _vec(freq, (s.rope_dims // 2,), _F64, dev, "freq"),
+            _mat(y, shape, dt, dev, "qk_norm_rope y"), y.stride(0))
     return y
 
 
@@ -540,14 +541,14 @@ def qk_norm_rope_backward(x, dy, dx, q_heads, k_heads, seq=1, q_gain=None, k_gai
     and g_bias (float32, optional) are added to. dx may be dy. ws: a workspace of
     qk_norm_rope_workspace bytes (None: from torch's allocator)."""
     s = _qk_shapes(x, q_heads, k_heads, seq, q_gain is not None or k_gain is not None, eps, freq, pairs)
-    dh = (s.head_dim,)
+    dh, shape, dt, dev = (s.head_dim,), x.shape, x.dtype, x.get_device()
     ws, n = _workspace(ws, lib.paci_qk_norm_rope_workspace, s, x)
-    _launch(lib.paci_qk_norm_rope_backward, x, ctypes.byref(s), _mat(x, x.shape, x, "qk_norm_rope x"), x.stride(0),
-            _mat(dy, x.shape, x, "qk_norm_rope dy"), dy.stride(0), _vec(q_gain, dh, _F32, x, "q_gain"),
-            _vec(k_gain, dh, _F32, x, "k_gain"), _vec(pos, (s.tokens,), _I32, x, "pos"),
-            _vec(freq, (s.rope_dims // 2,), _F64, x, "freq"), _mat(dx, x.shape, x, "qk_norm_rope dx"), dx.stride(0),
-            _vec(g_q_gain, dh, _F32, x, "g_q_gain"), _vec(g_k_gain, dh, _F32, x, "g_k_gain"),
-            _vec(g_bias, (x.shape[1],), _F32, x, "g_bias"), ws.data_ptr(), n)
+    _launch(lib.paci_qk_norm_rope_backward, dev, ctypes.byref(s), _mat(x, shape, dt, dev, "qk_norm_rope x"), x.stride(0),
+            _mat(dy, shape, dt, dev, "qk_norm_rope dy"), dy.stride(0), _vec(q_gain, dh, _F32, dev, "q_gain"),
+            _vec(k_gain, dh, _F32, dev, "k_gain"), _vec(pos, (s.tokens,), _I32, dev, "pos"),
+            _vec(freq, (s.rope_dims // 2,), _F64, dev, "freq"), _mat(dx, shape, dt, dev, "qk_norm_rope dx"), dx.stride(0),
+            _vec(g_q_gain, dh, _F32, dev, "g_q_gain"), _vec(g_k_gain, dh, _F32, dev, "g_k_gain"),
+            _vec(g_bias, shape[1:], _F32, dev, "g_bias"), ws.data_ptr(), n)
     return dx
 
 
@@ -561,10 +562,10 @@ def _attn_shapes(q, batch, n_heads, table, max_distance):
 
 
 def _attn_inputs(s, q, k, v, table, bounds):
-    shape = q.shape
-    return (_mat(q, shape, q, "attention q"), q.stride(0), _mat(k, shape, q, "attention k"), k.stride(0),
-            _mat(v, shape, q, "attention v"), v.stride(0), _vec(table, (s.n_buckets, s.n_heads), _F32, q, "table"),
-            _vec(bounds, (s.n_buckets,), _I32, q, "bounds"))
+    shape, dt, dev = q.shape, q.dtype, q.get_device()
+    return (_mat(q, shape, dt, dev, "attention q"), q.stride(0), _mat(k, shape, dt, dev, "attention k"), k.stride(0),
+            _mat(v, shape, dt, dev, "attention v"), v.stride(0), _vec(table, (s.n_buckets, s.n_heads), _F32, dev, "table"),
+            _vec(bounds, (s.n_buckets,), _I32, dev, "bounds"))
 
 
 def attention(q, k, v, o, lse2, batch, n_heads, table=None, bounds=None, max_distance=0):
@@ -573,8 +574,9 @@ def attention(q, k, v, o, lse2, batch, n_heads, table=None, bounds=None, max_dis
     bias table [n_buckets, n_heads] float32 and its bounds [n_buckets] int32 (rel_bounds
     gives the usual ones), or without."""
     s = _attn_shapes(q, batch, n_heads, table, max_distance)
-    _launch(lib.paci_attn_forward, q, ctypes.byref(s), *_attn_inputs(s, q, k, v, table, bounds),
-            _vec(o, q.shape, q.dtype, q, "o"), _vec(lse2, (batch * n_heads, s.seq), _F32, q, "lse2"))
+    dev = q.get_device()
+    _launch(lib.paci_attn_forward, dev, ctypes.byref(s), *_attn_inputs(s, q, k, v, table, bounds),
+            _vec(o, q.shape, q.dtype, dev, "o"), _vec(lse2, (batch * n_heads, s.seq), _F32, dev, "lse2"))
     return o
 
 
@@ -589,13 +591,13 @@ def attention_backward(q, k, v, o, lse2, do, dq, dk, dv, batch, n_heads, table=N
     o and lse2; g_table (float32, optional) is added to. ws: a workspace of
     attention_workspace bytes (None: from torch's allocator)."""
     s = _attn_shapes(q, batch, n_heads, table, max_distance)
-    shape = q.shape
+    shape, dt, dev = q.shape, q.dtype, q.get_device()
     ws, n = _workspace(ws, lib.paci_attn_workspace, s, q)
-    _launch(lib.paci_attn_backward, q, ctypes.byref(s), *_attn_inputs(s, q, k, v, table, bounds),
-            _vec(o, shape, q.dtype, q, "o"), _vec(lse2, (batch * n_heads, s.seq), _F32, q, "lse2"),
-            _vec(do, shape, q.dtype, q, "do"), _mat(dq, shape, q, "dq"), dq.stride(0), _mat(dk, shape, q, "dk"), dk.stride(0),
-            _mat(dv, shape, q, "dv"), dv.stride(0), _vec(g_table, (s.n_buckets, n_heads), _F32, q, "g_table"),
-            ws.data_ptr(), n)
+    _launch(lib.paci_attn_backward, dev, ctypes.byref(s), *_attn_inputs(s, q, k, v, table, bounds),
+            _vec(o, shape, dt, dev, "o"), _vec(lse2, (batch * n_heads, s.seq), _F32, dev, "lse2"),
+            _vec(do, shape, dt, dev, "do"), _mat(dq, shape, dt, dev, "dq"), dq.stride(0), _mat(dk, shape, dt, dev, "dk"),
+            dk.stride(0), _mat(dv, shape, dt, dev, "dv"), dv.stride(0),
+            _vec(g_table, (s.n_buckets, n_heads), _F32, dev, "g_table"), ws.data_ptr(), n)
     return dq, dk, dv
 
 
