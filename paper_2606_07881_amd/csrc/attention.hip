@@ -898,7 +898,7 @@ template <int DH, bool SMALL = false> struct BwdRing {
 constexpr int PAIR_ROWS = 2;
 template <int DH>
 __global__ void __launch_bounds__(NT) attn_pairs_kernel(const bf16* o, const bf16* dO, const float* lse2, float* pairs,
-                                                         int S, int S_pad, int H, int d, int64_t rows, bool bias) {
+                                                         int S, int S_pad, int H, int d, int64_t rows) {
   constexpr int LPR = DH / 8;
   const int64_t gid = (int64_t)blockIdx.x * NT + threadIdx.x;
   const int64_t row0 = gid / LPR * PAIR_ROWS;  // row = token * H + h
@@ -922,8 +922,7 @@ __global__ void __launch_bounds__(NT) attn_pairs_kernel(const bf16* o, const bf1
     if (row < rows && part == 0) {
       const int64_t tok = row / H, bq = tok / S, q = tok % S;
       const int64_t bh = bq * H + row % H;
-      const float lq = lse2[bh * S + q];
-      pairs[(bh * S_pad + q) * 2] = bias ? query_lse<true>(lq) : lq;
+      pairs[(bh * S_pad + q) * 2] = lse2[bh * S + q];
       pairs[(bh * S_pad + q) * 2 + 1] = sum;
     }
   }
@@ -935,6 +934,43 @@ __global__ void __launch_bounds__(NT) attn_pairs_kernel(const bf16* o, const bf1
     pairs[(bh * S_pad + q) * 2] = 0.f;
     pairs[(bh * S_pad + q) * 2 + 1] = 0.f;
   }
+}
+
+// The same with a bias: D as the diagonal of the products dO o^T, one wavefront per 16 queries
+// of a head, in the steps in which the backward forms dP = dO V^T. A query that sees one key
+// has o = v; the two sums are then the same float and its dS is zero, as it has to be. D by
+// another order leaves the rounding of a sum (1e-7 of |dO v|), which is all that a table's
+// gradient holds where every query sees one key. bf16: (lse2, D) pairs, with +inf for the lse2
+// of a query that sees none, and zeros behind the sequence; fp32: D alone. A pass is no longer
+// for it: 8 x 1024 tokens, 16 heads of 64: 114.6 us, 115.0 with the kernel above; 2 x 777, 3 heads
+// of 64: 32.6, 33.5. Without a bias the kernels above stay, and with them their bits.
+template <typename T, int DH>
+__global__ void __launch_bounds__(NT) attn_bias_dsum_kernel(const T* o, const T* dO, const float* lse2, float* out, int S,
+                                                             int S_pad, int H, int d, int64_t tiles) {
+  constexpr int V = Vec<T>::V, STEPS = DH / (4 * V);
+  const int l = lane_id(), g = l >> 4, c = l & 15;
+  const int64_t tile = (int64_t)blockIdx.x * (NT / 64) + (threadIdx.x >> 6);   // (sequence, 16 queries, head)
+  if (tile >= tiles) return;
+  const int h = tile % H, q = (int)(tile / H % (S_pad / 16)) * 16 + c;
+  const int64_t b = tile / H / (S_pad / 16), bh = b * H + h;
+  const bool ok = q < S;
+  const int64_t off = (b * S + q) * d + h * DH + g * V;
+  u32x4 x[STEPS], y[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    x[s] = ok ? ld16(dO + off + s * 4 * V) : u32x4{0, 0, 0, 0};
+    y[s] = ok ? ld16(o + off + s * 4 * V) : u32x4{0, 0, 0, 0};
+  }
+  const float lq = ok ? lse2[bh * S + q] : 0.f;
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) mma_step<T>(acc, x[s], y[s]);
+  if ((c >> 2) != g) return;   // lane (g, c) holds rows 4 g + r of column c
+  const float D = (c & 2) ? ((c & 1) ? acc[3] : acc[2]) : ((c & 1) ? acc[1] : acc[0]);
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<float2*>(out + (bh * S_pad + q) * 2) = make_float2(query_lse<true>(lq), D);
+  else if (ok)
+    out[bh * S + q] = D;
 }
 
 // Column sums of the gradient tiles a workgroup holds, for the bias gradient of
@@ -1495,15 +1531,24 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
   BiasArgs ba = bias_args(a);
   if (a.table && gr.g_table) ba.part = bias_ws;
   const int64_t rows = (int64_t)mu * S * H;
+  auto bias_dsum = [&](int S_pad) {
+    const int64_t tiles = (int64_t)mu * H * (S_pad / 16);
+    hipLaunchKernelGGL((attn_bias_dsum_kernel<T, DH>), dim3((unsigned)((tiles + NT / 64 - 1) / (NT / 64))), dim3(NT), 0, st,
+                       reinterpret_cast<const T*>(o), g, lse2, ws, S, S_pad, H, d, tiles);
+  };
   auto launch = [&](auto bias) {
     constexpr bool B = decltype(bias)::value;
     if constexpr (sizeof(T) == 2) {
       const int S_pad = (S + 63) / 64 * 64;
-      const int64_t threads = (rows + PAIR_ROWS - 1) / PAIR_ROWS * (DH / 8);
-      const int64_t pad_threads = (int64_t)mu * H * (S_pad - S);
-      const int64_t grid_threads = threads > pad_threads ? threads : pad_threads;
-      hipLaunchKernelGGL((attn_pairs_kernel<DH>), dim3((unsigned)((grid_threads + NT - 1) / NT)), dim3(NT), 0, st,
-                         reinterpret_cast<const bf16*>(o), g, lse2, ws, S, S_pad, H, d, rows, B);
+      if constexpr (!B) {
+        const int64_t threads = (rows + PAIR_ROWS - 1) / PAIR_ROWS * (DH / 8);
+        const int64_t pad_threads = (int64_t)mu * H * (S_pad - S);
+        const int64_t grid_threads = threads > pad_threads ? threads : pad_threads;
+        hipLaunchKernelGGL((attn_pairs_kernel<DH>), dim3((unsigned)((grid_threads + NT - 1) / NT)), dim3(NT), 0, st,
+                           reinterpret_cast<const bf16*>(o), g, lse2, ws, S, S_pad, H, d, rows);
+      } else {
+        bias_dsum(S_pad);
+      }
       hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
       auto go = [&](auto small) {
@@ -1519,9 +1564,13 @@ hipError_t bwd_launch(const AttnArgs& a, const AttnGrads& gr, const void* o, con
       else go(std::false_type{});
       return hipGetLastError();
     } else {
-      const int64_t threads = rows * (DH / Vec<T>::V);
-      hipLaunchKernelGGL((attn_dsum_kernel<T, DH>), dim3((unsigned)((threads + NT - 1) / NT)), dim3(NT), 0, st,
-                         reinterpret_cast<const T*>(o), g, ws, S, H, d, rows);
+      if constexpr (!B) {
+        const int64_t threads = rows * (DH / Vec<T>::V);
+        hipLaunchKernelGGL((attn_dsum_kernel<T, DH>), dim3((unsigned)((threads + NT - 1) / NT)), dim3(NT), 0, st,
+                           reinterpret_cast<const T*>(o), g, ws, S, H, d, rows);
+      } else {
+        bias_dsum((S + 15) / 16 * 16);
+      }
       hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
       const int nkb = (S + BKV - 1) / BKV;
