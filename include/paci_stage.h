@@ -376,9 +376,11 @@ int paci_qk_norm_rope_backward(const paci_qk_shapes* s, const void* dev_x, int64
  *   o = softmax(q k^T / sqrt(head_dim) + table[bucket(i - j)][head]) v
  * over the keys j at or before each query i. bucket(n) is the number of
  * bounds[1 .. n_buckets - 1] at or below min(n, max_distance). Table entries at
- * or below -1e9 (-inf, the lowest float) hide their distances from that head;
- * a query with no key left has o = 0 and lse2 = -inf and passes no gradient on.
- * Finite entries above 1e9 count as 1e9. The operands are finite, in padding
+ * or below -2^15 (-inf, the lowest value of a type) hide their distances from
+ * that head; a query with no key left has o = 0 and lse2 = -inf and passes no
+ * gradient on. Finite entries above 2^15 count as 2^15. Within these bounds the
+ * backward's probabilities, taken from a 32-bit lse2, are off by a relative
+ * 2^-24 |lse2| at most beside the rounding of their scores. The operands are finite, in padding
  * rows too: a hidden or later key has probability zero, and zero times an
  * infinity or NaN is NaN in a product of matrices, so a non-finite row of k or
  * v can reach every query of its sequence that shares a block of keys with it.

@@ -8,7 +8,8 @@ The paper's stages use neither; both are options of this library's attention.
   position * freq[i].
 * Relative position bias: the score of query i and key j adds
   table[bucket(i - j), head], where bucket(n) counts the bounds[1:] at or below
-  min(n, max_distance); entries at or below -1e9 hide their distances.
+  min(n, max_distance); entries at or below -2^15 hide their distances, larger ones than
+  2^15 count as it.
 """
 import numpy as np
 
@@ -71,7 +72,8 @@ def buckets(bnd, max_distance, S):
 
 def bias_by_distance(table, bnd, max_distance, S):
     """[H, S] bias of each head at every distance (hidden ones -inf)."""
-    t = np.where(np.asarray(table) <= -1e9, -np.inf, np.asarray(table, np.float64))
+    t = np.minimum(np.asarray(table, np.float64), 2.0 ** 15)
+    t[t <= -2.0 ** 15] = -np.inf
     return t[buckets(bnd, max_distance, S)].T
 
 

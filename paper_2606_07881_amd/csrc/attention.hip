@@ -56,9 +56,11 @@ template <typename T> struct GradView {
 // reads the last value everywhere; a path of its own for such blocks, with the one value in
 // the exponent's constant, was no faster (backward 116 against 113 us at 8 x 1024 tokens, 16
 // heads of 64; 385 against 372 at 4 x 2048, 16 heads of 128, max_distance 256).
-// Entries at or below HIDDEN hide their distances (-inf), larger ones than MOST count as it:
-// the running maximum m of a row is rounded, so its largest exponent can be off zero by
-// 2^-24 |m|, which cancels in the quotient as long as 2 to that power is a float.
+// Entries at or below HIDDEN hide their distances (-inf), larger ones than MOST count as it.
+// Both bounds are where the backward still holds: it forms P = 2^(x - lse2) from one float
+// lse2, whose rounding is half a step at |entry| log2 e, so P is off by the factor
+// 2^(2^-24 |lse2|) at worst: 1.0014 within 2^15 (a bf16 half step is 0.0039), 1.04 at 1e6, 6 at
+// 1e8. (The forward's own error of that kind is in the sum as in its terms and cancels.)
 struct BiasArgs {
   const float* table;      // [n_buckets][H]
   const int32_t* bounds;   // first distance of every bucket, ascending
@@ -67,7 +69,7 @@ struct BiasArgs {
   float* part;             // dQ wavefronts: sums of dS by distance, [H][batch][wavefront][max_distance + 1], or null
 };
 constexpr int BIAS_FRONT = 80, BIAS_TAIL = 128;   // distances below 0 (masked keys) and above max_distance inside a window
-constexpr float BIAS_HIDDEN = -1e9f, BIAS_MOST = 1e9f;
+constexpr float BIAS_HIDDEN = -32768.f, BIAS_MOST = 32768.f;
 __host__ __device__ __forceinline__ int bias_len(int max_distance) { return BIAS_FRONT + max_distance + BIAS_TAIL; }
 // A dQ wavefront of SUB query tiles moves its diagonal sums through 4 rows of DiagRow floats of LDS.
 template <int SUB> struct DiagRow { static constexpr int N = 16 * (SUB + 5), FLOATS = 4 * N; };

@@ -167,7 +167,7 @@ hipError_t rotary(const RotArgs& r, bool bwd, hipStream_t st);
 // mu sequences of S tokens, H heads of dh; row t of q at q + t ldq (elements), head h at
 // + h dh, likewise k and v. With a table, score (i, j) adds table[bucket(i - j)][h], where
 // bucket(n) counts the bounds[1 .. n_buckets - 1] at or below min(n, max_distance);
-// entries at or below -1e9 hide their distances, finite ones above 1e9 count as 1e9.
+// entries at or below -2^15 hide their distances, finite ones above 2^15 count as 2^15.
 constexpr int MAX_BUCKETS = 256, MAX_DISTANCE = 512;
 struct AttnArgs {
   DType dt = DT_F32;

@@ -149,3 +149,9 @@ def test_stage_gradients_match_central_differences(kind, over):
             arr[ix] = old
             fd = (a - b) / (2 * h)
             assert abs(grads[name][ix] - fd) <= 1e-7 * max(1.0, abs(fd)) + 1e-8, (name, ix)
+
+
+def test_entries_count_within_2_to_the_15():
+    t = np.float32([[-3e38], [-32768.0], [-32767.0], [32767.0], [32769.0], [3e38]])
+    got = positions.bias_by_distance(t, list(range(6)), 5, 6)[0]
+    assert got.tolist() == [-np.inf, -np.inf, -32767.0, 32767.0, 32768.0, 32768.0]
