@@ -153,3 +153,40 @@ def test_entries_at_or_below_the_lowest_hide(binding, dtype, entry):
     c = _with_table((2, 100, 2, 64), dtype, table)
     assert np.isneginf(c.lse2.reshape(2, 2, 100)[:, 0]).all()
     _check_probabilities(binding, c)
+
+
+# ---- layouts ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("buckets", [0, 8])
+@pytest.mark.parametrize("shape,dtype", [((2, 140, 2, 64), "bf16"), ((2, 140, 2, 64), "fp32"), ((1, 90, 3, 32), "bf16"),
+                                         ((1, 90, 3, 32), "fp32"), ((2, 75, 2, 128), "bf16"), ((9, 200, 16, 64), "bf16")], ids=str)
+def test_the_operands_layout_does_not_matter(binding, shape, dtype, buckets):
+    """The thirds of a fused projection (and of its gradient) against buffers of their own with wider rows, other orders and
+    NaN around them: the same bits, with a bias and without."""
+    import torch
+    c = Attn((*shape, buckets, 7, ""), dtype, 17)
+    act = torch.bfloat16 if dtype == "bf16" else torch.float32
+    kw = dict(batch=c.B, n_heads=c.H)
+    if buckets:
+        kw.update(table=dev(c.table), bounds=torch.from_numpy(c.bounds).cuda(), max_distance=c.md)
+
+    def chain(operands, grads):
+        o, lse2 = torch.empty(c.T, c.d, device="cuda", dtype=act), torch.empty(c.B * c.H, c.S, device="cuda")
+        g_table = torch.zeros(buckets, c.H, device="cuda") if buckets else None
+        binding.attention(*operands, o, lse2, **kw)
+        binding.attention_backward(*operands, o, lse2, dev(c.do, dtype), *grads, g_table=g_table, **kw)
+        return [o, lse2, *grads] + ([g_table] if buckets else [])
+
+    def apart(pads):
+        return [torch.full((c.T, c.d + p), float("nan"), device="cuda", dtype=act)[:, 8:8 + c.d] for p in pads]
+    qkv = dev(c.qkv, dtype)
+    fused = chain(qkv.split(c.d, 1), torch.empty_like(qkv).split(c.d, 1))
+    operands = apart((8, 40, 24))
+    for t, a in zip(operands, (c.q, c.k, c.v)):
+        t.copy_(dev(a, dtype))
+    other = chain(operands, apart((56, 8, 16)))
+    vk = torch.empty(c.T, 2 * c.d, device="cuda", dtype=act)   # v before k, q alone
+    vk[:, :c.d], vk[:, c.d:] = dev(c.v, dtype), dev(c.k, dtype)
+    dkv = torch.empty_like(vk)
+    third = chain([dev(c.q, dtype), vk[:, c.d:], vk[:, :c.d]], [torch.empty(c.T, c.d, device="cuda", dtype=act), dkv[:, c.d:], dkv[:, :c.d]])
+    for i, (x, y, z) in enumerate(zip(fused, other, third)):
+        assert torch.isfinite(x).all() and torch.equal(x, y) and torch.equal(x, z), i
