@@ -428,8 +428,13 @@ class Stage:
 # written for few Python operations: a small call costs more here than on the GPU.
 _TORCH_DTYPES = {torch.bfloat16: BF16, torch.float32: FP32}
 _F32, _I32, _F64 = torch.float32, torch.int32, torch.float64
-# the current stream's handle; torch.cuda.current_stream makes a Stream object around it (1 us of a 9 us call)
-_raw_stream = torch._C._cuda_getCurrentRawStream
+def _stream_handle(dev):
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+# the current stream's handle without the Stream object that torch.cuda.current_stream makes around it (1 us of a 9 us
+# call); a torch that lacks this private name has the other way, and one without devices this module's host calls
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_handle)
 _INT_MAX = 2 ** 31 - 1   # sizes are int32 in the C structures, which would keep the low bits of larger ones
 
 

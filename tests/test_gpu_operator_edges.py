@@ -190,3 +190,12 @@ def test_the_operands_layout_does_not_matter(binding, shape, dtype, buckets):
     third = chain([dev(c.q, dtype), vk[:, c.d:], vk[:, :c.d]], [torch.empty(c.T, c.d, device="cuda", dtype=act), dkv[:, c.d:], dkv[:, :c.d]])
     for i, (x, y, z) in enumerate(zip(fused, other, third)):
         assert torch.isfinite(x).all() and torch.equal(x, y) and torch.equal(x, z), i
+
+
+# ---- streams ----------------------------------------------------------------------------------
+def test_both_ways_to_the_current_stream_agree(binding):
+    import torch
+    dev_index = torch.cuda.current_device()
+    for st in (torch.cuda.current_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(st):
+            assert binding._raw_stream(dev_index) == binding._stream_handle(dev_index) == st.cuda_stream

@@ -219,3 +219,21 @@ def test_stage_options_are_checked_and_listed():
     assert arena(qk_norm=0, rope_dims=0, rel_buckets=0) == 0
     extra = with_options - out.value
     assert 4 * 6 * T * 2 * d * 2 <= extra <= 4 * 6 * T * 2 * d * 2 + (24 << 20)
+
+
+# ---- the binding's import -----------------------------------------------------------------
+def test_the_binding_needs_no_private_name_of_torch(root):
+    """A torch without device support lacks the raw stream call: the module's host calls still work."""
+    import subprocess
+    import sys
+    code = """
+import sys
+sys.path.insert(0, {root!r})
+import torch
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):
+    del torch._C._cuda_getCurrentRawStream
+from paper_2606_07881_amd import binding
+print(len(binding.rel_bounds(32, 128)), binding._raw_stream is binding._stream_handle)
+""".format(root=root)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.split() == ["32", "True"], r.stdout + r.stderr
