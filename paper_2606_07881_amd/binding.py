@@ -424,7 +424,9 @@ class Stage:
 # ---- attention operators (device) ------------------------------------------------------------
 # Each runs on the tensors' device and its current torch stream. Matrices are
 # [rows, columns] with contiguous rows (any row stride the C ABI admits, e.g. a
-# column range of a fused projection); vectors are contiguous. The checks are
+# column range of a fused projection); vectors are contiguous. They know nothing of
+# autograd: results are written into the caller's tensors and carry no graph, also
+# where an operand requires gradients; the *_backward calls give those. The checks are
 # written for few Python operations: a small call costs more here than on the GPU.
 _TORCH_DTYPES = {torch.bfloat16: BF16, torch.float32: FP32}
 _F32, _I32, _F64 = torch.float32, torch.int32, torch.float64
@@ -525,7 +527,8 @@ def qk_norm_rope(x, y, q_heads, k_heads, seq=1, q_gain=None, k_gain=None, eps=1e
     """paci_qk_norm_rope_forward: y = the normalised and rotated heads of x
     [tokens, (q_heads + k_heads) * head_dim]. Gains ([head_dim] float32): norm, None:
     no norm. freq ([rope_dims / 2] float64): rotation, None: none. pos ([tokens] int32)
-    or, without it, row % seq. y may be x."""
+    or, without it, row % seq. y may be x. y carries no autograd graph:
+    qk_norm_rope_backward gives the gradients."""
     s = _qk_shapes(x, q_heads, k_heads, seq, q_gain is not None or k_gain is not None, eps, freq, pairs)
     dh, shape, dt, dev = (s.head_dim,), x.shape, x.dtype, x.get_device()
     _launch(lib.paci_qk_norm_rope_forward, dev, ctypes.byref(s), _mat(x, shape, dt, dev, "qk_norm_rope x"), x.stride(0),
@@ -577,7 +580,8 @@ def attention(q, k, v, o, lse2, batch, n_heads, table=None, bounds=None, max_dis
     """paci_attn_forward: causal attention of q, k and v [batch * seq, n_heads * head_dim]
     into o (contiguous) and lse2 [batch * n_heads, seq] float32, with the relative position
     bias table [n_buckets, n_heads] float32 and its bounds [n_buckets] int32 (rel_bounds
-    gives the usual ones), or without."""
+    gives the usual ones), or without. o and lse2 carry no autograd graph:
+    attention_backward gives the gradients."""
     s = _attn_shapes(q, batch, n_heads, table, max_distance)
     dev = q.get_device()
     _launch(lib.paci_attn_forward, dev, ctypes.byref(s), *_attn_inputs(s, q, k, v, table, bounds),

@@ -2,7 +2,7 @@
 //
 // q, k and v are rows of H * dh elements with a row stride each (side by side in
 // the fused projection, or q and k in a buffer of their own) and are read in
-// place. Blocks of 64 keys (and of 64 or 32 queries) are staged in LDS, and every
+// place. Blocks of 64 keys (and of 64 queries) are staged in LDS, and every
 // product is an MFMA chain in the convention of device_common.hpp.
 //
 // Forward (one workgroup per (sequence, head, 64 queries); 4 wavefronts of 16
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__((FwdRing<DH, SMALL>::NTF), 2) attn_fwd_ring_ke
       scores(kb + 1, nxt);
       softmax(std::false_type{}, kb, cur, pf);
       // interleave: the fragment reads first, then one MFMA per few ALU instructions
-      // (with a bias its reads too: 133 against 140 us at 4 x 2048 tokens, 16 heads of 128)
+      // (with a bias its reads too: 122 against 126 us a pass at 4 x 2048 tokens, 16 heads of 128)
       __builtin_amdgcn_sched_group_barrier(0x100, 4 * KS + (BIAS ? 2 * (QS + 3) : 0), 0);
 #pragma unroll
       for (int i = 0; i < 4 * KS * QS; ++i) {
@@ -640,7 +640,7 @@ __global__ void __launch_bounds__(NT) attn_dsum_kernel(const T* o, const T* dO, 
 // ---------------------------------------------------------------------------------------
 // The fp32 backward's two kinds of workgroup (tiles: BwdTiles<T, DH>::SLOTS slots of LDS).
 template <typename T, int DH> struct BwdTiles {
-  static constexpr int BQ = (DH >= 128) ? 32 : 64;   // queries per staged block of dK/dV (LDS budget)
+  static constexpr int BQ = 64;                      // queries per staged block of dK/dV
   static constexpr int TILE = DH / Vec<T>::V * 64;   // 64 rows of a head
   static constexpr int DKDV = 4 * DH / Vec<T>::V * BQ + BQ / 2, DQ = 3 * TILE;
   static constexpr int SLOTS = DKDV > DQ ? DKDV : DQ;
@@ -1606,7 +1606,9 @@ bool attn_args_ok(const AttnArgs& a) {
 
 }  // namespace
 
-// fp32 at head_dim 128 would exceed the 64 KiB LDS budget of its tilings
+// fp32 stops at head_dim 64: its backward's tiles take 65 KiB there and up to 11 KiB of bias, two
+// workgroups to a CU's 160 KiB. At 128 the tiles alone would be 129 KiB, one workgroup of 4
+// wavefronts to a CU.
 hipError_t attn_fwd(const AttnArgs& a, void* o, float* lse2, hipStream_t st) {
   if (!attn_args_ok(a)) return hipErrorInvalidValue;
   if (a.dt == DT_BF16) {

@@ -18,9 +18,10 @@
 // gains and, in the backward, its sums for the gains and for the column sums of
 // dx stay in registers. The tokens of a workgroup are taken U to a thread at a
 // time: their loads are issued first, then the workgroup computes the angles of
-// those tokens once for all heads, into LDS. Measured (kernel): 8192 tokens of 16 + 16
-// heads of 64, bf16: forward 14.4 us, 4.7 TB/s; backward 24 us, 4.2 TB/s, and 4 us
-// for the sums' second launch (a 1 GiB copy reaches 5.1 TB/s on this card).
+// those tokens once for all heads, into LDS. Measured, a pass over 8192 tokens of 16 + 16
+// heads of 64 in bf16: forward 15.2 us on one set of buffers, part of which stays in the
+// 256 MB cache (a copy of the same 67 MB: 10.2), 19.0 on eight sets in turn, from HBM
+// (copy 14.1); backward 28.6 and 34.2 us, 4 of them the sums' second launch.
 //
 // Angles: pos * freq in 64 bits and reduced to a fraction of a turn there (a 32-bit
 // product is off by 0.06 at position 10^6); the sine and cosine of the fraction
@@ -341,8 +342,8 @@ __global__ void __launch_bounds__(NT) rotary_sums_kernel(const float* __restrict
   if (out != nullptr) out[gain && col >= dh ? col - dh : col] += s;
 }
 
-// The launch of a pass. U tokens in flight per thread: 64 bytes a vector pair in the
-// forward (4 in bf16, 2 in fp32), half that in the backward, which reads two rows and
+// The launch of a pass. U tokens in flight per thread: 128 bytes a lane in the forward
+// (4 tokens in bf16, 2 in fp32), half that in the backward, which reads two rows and
 // holds its sums (with 4 it takes 256 registers and spills to the second file: 13 us more
 // at 8192 tokens of 16 + 16 heads of 64 in bf16; 1 is as fast there). Backward workgroups
 // each leave a row of sums, so there are few: two of 256 threads to a CU (27.4 us there;
