@@ -517,7 +517,7 @@ def _qk_shapes(x, q_heads, k_heads, seq, norm, eps, freq, pairs):
     dt = _operand(x, "qk_norm_rope x")
     tokens, cols = x.shape
     heads = q_heads + k_heads
-    if heads < 1 or min(q_heads, k_heads) < 0 or cols % heads or pairs not in ROPE_PAIRS or max(tokens, cols, seq) > _INT_MAX:
+    if heads < 1 or min(q_heads, k_heads, seq) < 0 or cols % heads or pairs not in ROPE_PAIRS or max(tokens, cols, seq) > _INT_MAX:
         _refuse(f"qk_norm_rope: {cols} columns of {heads} heads, pairs {pairs!r}")
     return PaciQkShapes(dt, tokens, seq, q_heads, k_heads, cols // heads, norm, eps, 0 if freq is None else 2 * freq.numel(),
                         ROPE_PAIRS[pairs])
@@ -563,7 +563,8 @@ def qk_norm_rope_backward(x, dy, dx, q_heads, k_heads, seq=1, q_gain=None, k_gai
 def _attn_shapes(q, batch, n_heads, table, max_distance):
     dt = _operand(q, "attention q")
     T, d = q.shape
-    if batch < 0 or n_heads < 1 or d % n_heads or (T % batch if batch else T) or max(T, d, batch, max_distance) > _INT_MAX:
+    if (min(batch, max_distance) < 0 or n_heads < 1 or d % n_heads or (T % batch if batch else T) or
+            max(T, d, batch, max_distance) > _INT_MAX):
         _refuse(f"attention: {(T, d)} is not {batch} sequences of {n_heads} heads")
     return PaciAttnShapes(dt, batch, T // batch if batch else 0, n_heads, d // n_heads, 0 if table is None else table.shape[0],
                           max_distance)

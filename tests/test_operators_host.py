@@ -221,6 +221,16 @@ def test_stage_options_are_checked_and_listed():
     assert 4 * 6 * T * 2 * d * 2 <= extra <= 4 * 6 * T * 2 * d * 2 + (24 << 20)
 
 
+def test_binding_refuses_negative_sizes_beyond_the_c_types():
+    """The low 32 bits of these are sizes that the C calls take."""
+    big = 2 ** 32
+    for call in (lambda: binding.qk_norm_rope_workspace(Shape(4, 128), 1, 1, seq=4 - big),
+                 lambda: binding.attention_workspace(Shape(4, 128), 1, 2, table=torch.zeros(8, 2), max_distance=32 - big)):
+        with pytest.raises(binding.PaciError) as e:
+            call()
+        assert e.value.code == INVAL
+
+
 # ---- the binding's import -----------------------------------------------------------------
 def test_the_binding_needs_no_private_name_of_torch(root):
     """A torch without device support lacks the raw stream call: the module's host calls still work."""
