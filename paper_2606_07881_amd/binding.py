@@ -440,8 +440,15 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_handle)
 _INT_MAX = 2 ** 31 - 1   # sizes are int32 in the C structures, which would keep the low bits of larger ones
 
 
+def _int32(what, *sizes):
+    """ctypes passes the low 32 bits of an int: others than these would make the C call fill more than the array holds."""
+    if max(sizes) > _INT_MAX or min(sizes) < -_INT_MAX:
+        _refuse(f"{what}: {sizes}")
+
+
 def rope_freqs(theta, rope_dims):
     """paci_rope_freqs: theta^(-2 i / rope_dims), i < rope_dims / 2, as a float64 array."""
+    _int32("rope_freqs", rope_dims)
     f = np.zeros(max(rope_dims // 2, 1), np.float64)
     _check(lib.paci_rope_freqs(float(theta), rope_dims, f.ctypes.data_as(ctypes.POINTER(ctypes.c_double))),
            "paci_rope_freqs")
@@ -450,6 +457,7 @@ def rope_freqs(theta, rope_dims):
 
 def rel_bounds(n_buckets, max_distance):
     """paci_rel_bounds: the first distance of every bucket, as an int32 array."""
+    _int32("rel_bounds", n_buckets, max_distance)
     b = np.zeros(max(n_buckets, 1), np.int32)
     _check(lib.paci_rel_bounds(n_buckets, max_distance, b.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))),
            "paci_rel_bounds")

@@ -231,6 +231,17 @@ def test_binding_refuses_negative_sizes_beyond_the_c_types():
         assert e.value.code == INVAL
 
 
+def test_host_calls_refuse_sizes_beyond_the_c_types():
+    """The C calls would see 64 dimensions and 32 buckets, and fill arrays made for the sizes given."""
+    big = 2 ** 32
+    for call in (lambda: binding.rope_freqs(1e4, 64 - big), lambda: binding.rope_freqs(1e4, 64 + big),
+                 lambda: binding.rel_bounds(32 - big, 128), lambda: binding.rel_bounds(32 + big, 128),
+                 lambda: binding.rel_bounds(32, 128 + big), lambda: binding.rel_bounds(32, 128 - big)):
+        with pytest.raises(binding.PaciError) as e:
+            call()
+        assert e.value.code == INVAL
+
+
 # ---- the binding's import -----------------------------------------------------------------
 def test_the_binding_needs_no_private_name_of_torch(root):
     """A torch without device support lacks the raw stream call: the module's host calls still work."""
