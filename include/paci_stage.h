@@ -114,7 +114,8 @@ typedef struct paci_shapes {
   int32_t rel_buckets;  /* relative position bias: rows of each block's table rel [rel_buckets, n_heads], a
                            multiple of 8 up to 256, with the bounds of paci_rel_bounds; 0: none. A backward
                            differentiates the probabilities of its forward, so every micro-batch in
-                           flight keeps the tables its forward read, as it keeps its activations */
+                           flight keeps the tables its forward read, as it keeps its activations
+                           (a checkpointed stage: those of the forward that its backward recomputes) */
   int32_t rel_max_distance; /* rel_buckets / 2 < rel_max_distance <= 512 */
 } paci_shapes;
 
@@ -416,7 +417,8 @@ int paci_attn_forward(const paci_attn_shapes* s, const void* dev_q, int64_t ld_q
  * o and lse2: with P = 2^(score log2 e - lse2) and dS = P (do v^T - rowsum(do o)),
  * dq = dS k / sqrt(head_dim), dk = dS^T q / sqrt(head_dim), dv = P^T do, and
  * dev_g_table[b][h] (fp32 [n_buckets, n_heads], nullable) += the sum of dS over
- * the pairs of bucket b. dq, dk and dv have row strides and must not overlap an
+ * the pairs of bucket b. With a bias, dS of a query that sees one key is exactly
+ * zero. dq, dk and dv have row strides and must not overlap an
  * operand or each other. dev_ws: paci_attn_workspace bytes, 16-byte aligned. Errors as above. */
 int paci_attn_workspace(const paci_attn_shapes* s, size_t* bytes);
 int paci_attn_backward(const paci_attn_shapes* s, const void* dev_q, int64_t ld_q, const void* dev_k, int64_t ld_k,
