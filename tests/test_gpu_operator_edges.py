@@ -61,6 +61,23 @@ def test_a_query_that_sees_one_key_has_no_score_gradient(binding, shape, dtype):
     check(c.split(dv), want, (half_step(dtype) + 128 * U32) * np.abs(want), "dv")
 
 
+@pytest.mark.parametrize("entry", [-3e4, 3e4])
+@pytest.mark.parametrize("shape,dtype", [((700, 1, 2, 64), "bf16"), ((600, 1, 3, 32), "fp32"), ((2, 150, 3, 64), "fp32"),
+                                         ((9, 200, 16, 64), "bf16"), ((5, 90, 3, 128), "bf16")], ids=str)
+def test_nor_at_the_largest_entries(binding, shape, dtype, entry):
+    """There the forward's probability can be off one by 2^-9, and the sum it is divided by with it."""
+    B, S, H, dh = shape
+    far = 0 if S == 1 else 3
+    c = Attn((B, S, H, dh, 8, 7, ""), dtype, 18)
+    c.bounds = np.arange(8, dtype=np.int32)
+    c.table[:] = -np.inf
+    c.table[far] = np.float32(entry + np.random.default_rng(19).standard_normal(H))
+    o, _, dq, dk, _, g_table = run(binding, c)
+    assert np.array_equal(c.split(o)[:, :, far:], c.split(c.v)[:, :, :S - far])
+    for name, g in (("dq", dq), ("dk", dk), ("g_table", g_table)):
+        assert not g.any(), name
+
+
 # ---- large entries ----------------------------------------------------------------------------
 def _with_table(shape, dtype, table):
     """An Attn case with a bucket per distance (7 and more share the last) and this table."""
